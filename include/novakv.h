@@ -330,6 +330,104 @@ novakv_status novakv_decode_attention_noalloc(novakv_ctx* ctx, int layer, const 
     const int32_t* page_table, int max_pages_per_seq, const int32_t* seq_lens, int batch,
     float sm_scale, void* out, int out_is_fp32, novakv_stream stream);
 
+/* ---- between the QKV projection and the cache ------------------------------------------------ */
+
+/*
+ * Norm and rotation of queries and keys, for each head x of d channels:
+ *     y = x / sqrt(mean_i x_i^2 + eps) * weight                       if a weight is given
+ *     (a, b) -> amplitude * (a cos t - b sin t, b cos t + a sin t)    t = position * inv_freq[i], i < rot_dim / 2
+ * Channels a, b of pair i are i and i + rot_dim / 2, or 2 i and 2 i + 1 if `interleaved`; channels from rot_dim on are not
+ * rotated.  The angle is formed in binary64 (far positions), the rest in binary32 (keys of the 4-bit cache: binary64), and the
+ * result is rounded to bf16 once.  The struct is read during the call; the device memory it names stays the caller's.
+ *   inv_freq   device float32 [rot_dim / 2]; rot_dim 0 (inv_freq may be NULL): no rotation
+ *   rot_dim    a multiple of 16, at most d (NOVAKV_ESHAPE otherwise)
+ *   amplitude  factor on cos and sin (the attention factor of extended contexts), 1 otherwise
+ *   q_weight, k_weight  device bf16 [d], NULL: that side is not normalised
+ */
+typedef struct {
+    const float* inv_freq;
+    const void* q_weight;
+    const void* k_weight;
+    int rot_dim;
+    int interleaved;
+    float amplitude;
+    float eps;
+} novakv_qk_transform;
+
+/*
+ * The transform alone, in front of a cache whose append takes keys as they are (novakv_encode_append, novakv_band_append, ...).
+ *   q [n_tokens][Hq][d], k [n_tokens][Hkv][d]  bf16; *_stride: elements from one token's rows to the next, at least heads * d (rows
+ *            cut out of a fused projection); heads of a token are contiguous.  Either may be NULL together with its output.
+ *   q_out, k_out  bf16, laid out the same way; an output may be its own input with the same stride, else they must not overlap
+ *   tok_pos  int32 [n_tokens], any value.  Rows 16-byte aligned (pointer and stride) are faster, others are taken.
+ * (novakv_decode_attention must not be the library call directly behind this one if it reads its q: see there.)
+ */
+novakv_status novakv_qk_norm_rope(novakv_ctx* ctx, const novakv_qk_transform* transform, const void* q, long long q_stride,
+    const void* k, long long k_stride, const int32_t* tok_pos, int n_tokens, void* q_out, long long q_out_stride,
+    void* k_out, long long k_out_stride, novakv_stream stream);
+
+/*
+ * Append to the BF16 cache that novakv_bf16_decode_attention reads (pools bf16 [n_pages][Hkv][64][d], 16-byte aligned): the
+ * keys go through `transform` (NULL: as they are) with position tok_pos[t], the values do not; both land in slot tok_pos[t] % 64
+ * of page page_table[tok_seq[t]][tok_pos[t] / 64], and seq_lens[tok_seq[t]] becomes max(seq_lens[tok_seq[t]], tok_pos[t] + 1).
+ * q, q_out: the tokens' queries through the same transform in the same pass; both NULL: none.
+ * Token lists, unused entries (tok_seq[t] = -1), skipped tokens and status bits are those of novakv_encode_append; the q_out
+ * row of an entry that is skipped is left as it was.  Two tokens of one call that name one slot leave either's bytes in it, or a
+ * mixture.
+ */
+novakv_status novakv_bf16_append(novakv_ctx* ctx, const novakv_qk_transform* transform, const void* k_new, long long k_stride,
+    const void* v_new, long long v_stride, const int32_t* tok_seq, const int32_t* tok_pos, int n_tokens,
+    void* k_pages_bf16, void* v_pages_bf16, int n_pages, const int32_t* page_table, int max_pages_per_seq, int n_seq,
+    int32_t* seq_lens, const void* q, long long q_stride, void* q_out, long long q_out_stride, novakv_stream stream);
+
+/* ---- 4-bit cache -------------------------------------------------------------------------------- */
+
+/*
+ * Keys and values as 4-bit integers with one bf16 (scale, zero) pair per token, KV head and 64 channels: 4.5 bits an element,
+ * no calibration.  Of a group x_0 .. x_63 in binary32 (keys: the transformed key in binary64, rounded to binary32):
+ *     zero  = bf16(min_i x_i)
+ *     scale = bf16((max_i x_i - zero) / 15)     binary32; replaced by 1 if not positive and finite
+ *     code_i = clamp(rint((x_i - zero) / scale), 0, 15)      binary32 subtraction and division, ties to even; NaN: 0
+ *     read:  x^_i = zero + scale * code_i
+ * A NaN in a group makes its zero, and so what is read of it, NaN.
+ * Two pools uint8 [n_pages][Hkv][chunk], 16-byte aligned, novakv_int4_page_bytes() per page and pool.  A chunk is two tiles of
+ * 32 tokens: [32][d / 2] code bytes, then [32][d / 64] pairs (scale, zero).  Byte c / 2 of a token's row holds the code of channel
+ * c in its low (even c) or high four bits, but the row's 16-byte pieces are permuted: piece p of token t of the tile is kept at
+ * p ^ (t / 2 % 4) (d = 128) or p ^ (t / 4 % 2) (d = 64).
+ *
+ * Append: arguments and rules of novakv_bf16_append.
+ */
+size_t novakv_int4_page_bytes(const novakv_ctx* ctx);
+novakv_status novakv_int4_append(novakv_ctx* ctx, const novakv_qk_transform* transform, const void* k_new, long long k_stride,
+    const void* v_new, long long v_stride, const int32_t* tok_seq, const int32_t* tok_pos, int n_tokens,
+    uint8_t* k_pages, uint8_t* v_pages, int n_pages, const int32_t* page_table, int max_pages_per_seq, int n_seq,
+    int32_t* seq_lens, const void* q, long long q_stride, void* q_out, long long q_out_stride, novakv_stream stream);
+
+/*
+ * Read-back: the values that the slots of the listed tokens stand for (a cached prefix in front of the attention of a prompt's
+ * next chunk), k_out, v_out [n_tokens][Hkv][d], 16-byte aligned, float32 if out_is_fp32 else bf16.  Lengths are not looked at: a
+ * slot that was never written gives arbitrary numbers.  Rows of unused entries (tok_seq[t] = -1) and of tokens and pages out of
+ * range (status bits) are left as they were.
+ */
+novakv_status novakv_int4_gather(novakv_ctx* ctx, const int32_t* tok_seq, const int32_t* tok_pos, int n_tokens,
+    const uint8_t* k_pages, const uint8_t* v_pages, int n_pages, const int32_t* page_table, int max_pages_per_seq, int n_seq,
+    void* k_out, void* v_out, int out_is_fp32, novakv_stream stream);
+
+/*
+ * Decode attention over the 4-bit cache: for each sequence softmax(sm_scale q k^^T) v^ over positions 0 .. seq_lens[b] - 1, or its
+ * last `window` ones (window > 0).  sink_logits: NULL, or float32 [Hq], one more logit per query head that has no value
+ * (natural-log units).  A sequence of length 0 yields zeros.  Sums, softmax statistics and accumulators are binary32; q is taken
+ * exactly, the weights that meet the codes have 22 bits.
+ *   q    bf16 [batch][Hq][d], 16-byte aligned; out [batch][Hq][d], float32 if out_is_fp32 else bf16
+ *   workspace  novakv_int4_workspace_bytes(ctx, batch) bytes, 256-byte aligned; contents are scratch
+ * A bad page id is replaced by page 0 and a bad length clamped (status bits).  A wait that gives up (novakv_debug_set_wait_limit)
+ * sets NOVAKV_DEV_WAIT_TIMEOUT and leaves the call's output unspecified.  novakv_debug_set_scan_ctas applies.
+ */
+size_t novakv_int4_workspace_bytes(const novakv_ctx* ctx, int batch);
+novakv_status novakv_int4_decode_attention(novakv_ctx* ctx, const void* q, const uint8_t* k_pages, const uint8_t* v_pages,
+    int n_pages, const int32_t* page_table, int max_pages_per_seq, const int32_t* seq_lens, int batch, float sm_scale, int window,
+    const float* sink_logits, void* out, int out_is_fp32, void* workspace, size_t workspace_bytes, novakv_stream stream);
+
 /* Synchronises `stream`, returns the device status word in *word and clears it. */
 novakv_status novakv_last_device_status(novakv_ctx* ctx, novakv_stream stream, uint32_t* word);
 

@@ -9,7 +9,7 @@ PyTorch fallback: if the shared library is missing or a call returns an error st
 from __future__ import annotations
 
 import ctypes
-from ctypes import c_int, c_float, c_void_p, c_size_t, c_long, c_double, c_uint32, POINTER
+from ctypes import c_int, c_float, c_void_p, c_size_t, c_long, c_longlong, c_double, c_uint32, POINTER
 
 import numpy as np
 
@@ -28,6 +28,8 @@ EXPORTED = [
     "novakv_debug_set_segment_weight", "novakv_debug_set_fused_merge",
     "novakv_band_append_staging_bytes", "novakv_band_append", "novakv_debug_set_wait_limit",
     "novakv_debug_append_kernel_tokens",
+    "novakv_qk_norm_rope", "novakv_bf16_append", "novakv_int4_page_bytes", "novakv_int4_append", "novakv_int4_gather",
+    "novakv_int4_workspace_bytes", "novakv_int4_decode_attention",
 ]
 
 
@@ -42,6 +44,45 @@ class Config(ctypes.Structure):
 
 class CalibrationPtrs(ctypes.Structure):
     _fields_ = [(n, c_void_p) for n in ("rk", "rk_inv_t", "rv", "k_mean", "v_mean", "cb_k", "cb_v")]
+
+
+class _TransformStruct(ctypes.Structure):
+    _fields_ = [("inv_freq", c_void_p), ("q_weight", c_void_p), ("k_weight", c_void_p), ("rot_dim", c_int), ("interleaved", c_int),
+                ("amplitude", c_float), ("eps", c_float)]
+
+
+class QKTransform:
+    """Norm and rotation of a layer's queries and keys (``novakv_qk_transform``): kept by the program, passed to every call.
+
+    ``inv_freq``: float32 [rot_dim / 2] on the device, or None (no rotation); ``interleaved``: pairs (2 i, 2 i + 1) instead of
+    (i, i + rot_dim / 2); ``amplitude``: factor on cos and sin; ``q_weight`` / ``k_weight``: bf16 [head_dim], or None (no norm).
+    """
+
+    def __init__(self, inv_freq=None, *, interleaved=False, amplitude=1.0, q_weight=None, k_weight=None, eps=1e-6):
+        import torch
+        given = [t for t in (inv_freq, q_weight, k_weight) if t is not None]
+        if any(t.dim() != 1 or not t.is_contiguous() for t in given) or len({t.device for t in given}) > 1:
+            raise ValueError("inv_freq and the weights are contiguous vectors on one device")
+        if inv_freq is not None and inv_freq.dtype != torch.float32:
+            raise ValueError("inv_freq is float32")
+        if any(w is not None and w.dtype != torch.bfloat16 for w in (q_weight, k_weight)):
+            raise ValueError("the weights are bfloat16")
+        self.inv_freq, self.q_weight, self.k_weight = inv_freq, q_weight, k_weight       # (kept alive with the addresses)
+        self._struct = _TransformStruct(*(None if t is None else t.data_ptr() for t in (inv_freq, q_weight, k_weight)),
+                                        0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(interleaved)), amplitude, eps)
+        self._address = ctypes.addressof(self._struct)
+
+    def check(self, head_dim, device):
+        """The weights have to fit the context's heads, and everything its device."""
+        for w in (self.q_weight, self.k_weight):
+            if w is not None and w.numel() != head_dim:
+                raise ValueError("a weight has one element for each channel of a head")
+        for t in (self.inv_freq, self.q_weight, self.k_weight):
+            if t is not None and t.get_device() != device:
+                raise ValueError("a transform lies on the context's device")
+
+    def data_ptr(self):
+        return self._address
 
 
 _lib = None
@@ -119,6 +160,19 @@ def load_library(path=None):
     lib.novakv_bf16_decode_attention.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int,
                                                  c_void_p, c_int, c_float, c_int, c_void_p, c_int, c_void_p,
                                                  c_size_t, c_void_p]
+    lib.novakv_qk_norm_rope.argtypes = [c_void_p, c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_int, c_void_p, c_longlong,
+                                        c_void_p, c_longlong, c_void_p]
+    lib.novakv_int4_append.argtypes = lib.novakv_bf16_append.argtypes = [
+        c_void_p, c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_int, c_void_p, c_int, c_int,
+        c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p]
+    lib.novakv_int4_page_bytes.argtypes = [c_void_p]
+    lib.novakv_int4_page_bytes.restype = c_size_t
+    lib.novakv_int4_gather.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_int, c_void_p, c_int, c_int, c_void_p, c_void_p,
+                                       c_int, c_void_p]
+    lib.novakv_int4_workspace_bytes.argtypes = [c_void_p, c_int]
+    lib.novakv_int4_workspace_bytes.restype = c_size_t
+    lib.novakv_int4_decode_attention.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_void_p, c_int, c_float, c_int,
+                                                 c_void_p, c_void_p, c_int, c_void_p, c_size_t, c_void_p]
     lib.novakv_profile_enable.argtypes = [c_void_p, c_int]
     lib.novakv_profile_read.argtypes = [c_void_p, c_int, POINTER(c_double), POINTER(c_long)]
     lib.novakv_debug_append_kernel_tokens.argtypes = [c_void_p]
@@ -160,6 +214,14 @@ def _bind_calls(lib):
     return _novakv_calls.bind(lib._handle)
 
 
+def _bind_operators(lib, device, n_q_heads, n_kv_heads, head_dim):
+    """The calls around the BF16 and the 4-bit cache, which check the tensors they are given against the context."""
+    import torch
+
+    from . import _novakv_calls
+    return _novakv_calls.bind_operators(lib._handle, device, n_q_heads, n_kv_heads, head_dim, (torch.bfloat16, torch.int32, torch.uint8))
+
+
 class Context:
     """Owns a ``novakv_ctx``; methods carry the names of the C entry points."""
 
@@ -172,11 +234,26 @@ class Context:
         self.n_groups = head_dim // 4
         self._scale = float(head_dim) ** -0.5
         self._calls = _bind_calls(self.lib)
+        self._operators = _bind_operators(self.lib, device, n_q_heads, n_kv_heads, head_dim)
 
     def _call(self, name, *args):
         status = self._calls[name](self.handle.value, *args)
         if status != 0:
             _check(self.lib, status, name)
+
+    def _operate(self, name, *args):
+        status = self._operators[name](self.handle.value, *args)
+        if status != 0:
+            _check(self.lib, status, name)
+
+    def _transform(self, transform):
+        """The transform, looked over once for each context that it is used with."""
+        if transform is not None and getattr(transform, "_checked", None) != (self.head_dim, self.cfg.device):
+            if not isinstance(transform, QKTransform):
+                raise TypeError("transform: a QKTransform or None")
+            transform.check(self.head_dim, self.cfg.device)
+            transform._checked = (self.head_dim, self.cfg.device)
+        return transform
 
     def close(self):
         if self.handle:
@@ -287,6 +364,38 @@ class Context:
             self.handle, layer, _ptr(q), _ptr(k_pages), _ptr(v_pages), int(k_pages.shape[0]), _ptr(page_table),
             int(page_table.shape[1]), _ptr(seq_lens), int(q.shape[0]), scale, _ptr(out),
             1 if out.dtype == torch.float32 else 0, _stream()), "novakv_decode_attention_noalloc")
+
+    # -- between the projection and the cache; the 4-bit cache ---------------------------------
+    def novakv_qk_norm_rope(self, transform, q, k, tok_pos, q_out, k_out):
+        """Norms and rotation of q [n][Hq][d] and k [n][Hkv][d] (views with a token stride are taken; one side may be None)."""
+        self._operate("novakv_qk_norm_rope", self._transform(transform), q, k, tok_pos, q_out, k_out)
+
+    def novakv_bf16_append(self, transform, k_new, v_new, tok_seq, tok_pos, k_pages_bf16, v_pages_bf16, page_table, seq_lens,
+                           q=None, q_out=None):
+        """Append to the BF16 paged cache, keys (and q, if given) through ``transform`` on the way (None: as they are)."""
+        self._operate("novakv_bf16_append", self._transform(transform), k_new, v_new, tok_seq, tok_pos, k_pages_bf16, v_pages_bf16,
+                      page_table, seq_lens, q, q_out)
+
+    def novakv_int4_page_bytes(self):
+        return int(self.lib.novakv_int4_page_bytes(self.handle))
+
+    def novakv_int4_append(self, transform, k_new, v_new, tok_seq, tok_pos, k_pages, v_pages, page_table, seq_lens, q=None, q_out=None):
+        """The same into the 4-bit paged cache."""
+        self._operate("novakv_int4_append", self._transform(transform), k_new, v_new, tok_seq, tok_pos, k_pages, v_pages, page_table,
+                      seq_lens, q, q_out)
+
+    def novakv_int4_gather(self, tok_seq, tok_pos, k_pages, v_pages, page_table, k_out, v_out):
+        """The values that slots of the 4-bit cache stand for, as rows [n][Hkv][d] in bf16 or float32."""
+        self._operate("novakv_int4_gather", tok_seq, tok_pos, k_pages, v_pages, page_table, k_out, v_out)
+
+    def novakv_int4_workspace_bytes(self, batch):
+        return int(self.lib.novakv_int4_workspace_bytes(self.handle, batch))
+
+    def novakv_int4_decode_attention(self, q, k_pages, v_pages, page_table, seq_lens, out, workspace, sm_scale=None, window=0,
+                                     sink_logits=None):
+        """Decode step over the 4-bit cache; ``window`` > 0: the last so many positions; ``sink_logits`` float32 [Hq] or None."""
+        self._operate("novakv_int4_decode_attention", q, k_pages, v_pages, page_table, seq_lens, out, workspace,
+                      self._scale if sm_scale is None else sm_scale, window, sink_logits)
 
     def novakv_last_device_status(self):
         word = c_uint32(0)

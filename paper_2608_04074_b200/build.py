@@ -20,7 +20,7 @@ LIB_CALIB = PKG_DIR / "libnovakv_calib.so"
 LIB_CALLS = PKG_DIR / ("_novakv_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 CUDA_SOURCES = ["novakv_api.cu", "novakv_encode.cu", "novakv_prefill.cu", "novakv_decode.cu", "novakv_bf16_decode.cu",
-                "novakv_noalloc.cu"]
+                "novakv_noalloc.cu", "novakv_rotate.cu", "novakv_int4_decode.cu"]
 
 
 def _newer(target: Path, sources: list[Path]) -> bool:

@@ -125,3 +125,39 @@ def read_tokens(k_pool: np.ndarray, v_pool: np.ndarray, page_table_row: np.ndarr
         kidx[:, h, :] = k_pool[page, h, ko]
         vidx[:, h, :] = v_pool[page, h, vo]
     return kidx, vidx
+
+
+# ---- 4-bit cache: a (page, KV head) chunk is two tiles of 32 tokens, [32][d / 2] code bytes and [32][d / 64] (scale, zero) pairs
+INT4_TILE, INT4_GROUP = 32, 64
+
+
+def int4_chunk_bytes(d: int) -> int:
+    return PAGE_TOKENS * (d // 2 + d // INT4_GROUP * 4)
+
+
+def int4_code_offsets(d: int) -> np.ndarray:
+    """Byte of the chunk that holds channels 2 i and 2 i + 1 (low, high four bits) of token t, [64][d / 2]."""
+    t, i = np.arange(PAGE_TOKENS)[:, None], np.arange(d // 2)[None]
+    row = t % INT4_TILE
+    piece = (i // 16) ^ (row // 2 % 4 if d == 128 else row // 4 % 2)
+    return t // INT4_TILE * (int4_chunk_bytes(d) // 2) + row * (d // 2) + piece * 16 + i % 16
+
+
+def int4_pair_offsets(d: int) -> np.ndarray:
+    """First byte of the (scale, zero) pair of token t, channels 64 g .. 64 g + 63, [64][d / 64]."""
+    t, g = np.arange(PAGE_TOKENS)[:, None], np.arange(d // INT4_GROUP)[None]
+    return t // INT4_TILE * (int4_chunk_bytes(d) // 2) + INT4_TILE * d // 2 + (t % INT4_TILE * (d // INT4_GROUP) + g) * 4
+
+
+def int4_read_tokens(pool: np.ndarray, table_row: np.ndarray, hkv: int, d: int, pos0: int, n: int):
+    """(codes uint8 [n][Hkv][d], scale, zero float32 [n][Hkv][d / 64]) of positions pos0 .. of one sequence.
+    pool: uint8 [n_pages][Hkv * chunk]."""
+    pos = pos0 + np.arange(n)
+    chunk = pool.reshape(len(pool), hkv, int4_chunk_bytes(d))[table_row[pos // PAGE_TOKENS]]
+    slot = pos % PAGE_TOKENS
+    rows = np.take_along_axis(chunk, int4_code_offsets(d)[slot][:, None].repeat(hkv, 1), -1)
+    codes = np.stack([rows & 15, rows >> 4], -1).reshape(n, hkv, d)
+    at = int4_pair_offsets(d)[slot][:, None, :, None] + np.arange(4)
+    pairs = np.take_along_axis(chunk[:, :, None, :], at.repeat(hkv, 1), -1).astype(np.uint32)
+    scale, zero = ((pairs[..., i] | pairs[..., i + 1] << 8) << 16 for i in (0, 2))
+    return codes, np.ascontiguousarray(scale).view(np.float32), np.ascontiguousarray(zero).view(np.float32)

@@ -61,7 +61,7 @@ static const struct { const char* name; int n_args; param p[MAX_ARGS]; } entries
     [STEP_HOST_ASYNC] = {"novakv_step_host_async", 14, HOST_PARAMS},
 };
 
-static PyObject *s_data_ptr, *s_shape, *s_dtype, *s_nbytes;
+static PyObject *s_data_ptr, *s_shape, *s_dtype, *s_nbytes, *s_stride, *s_get_device, *s_is_contiguous;
 static PyObject *get_stream, *get_device, *float32;        /* given by setup() */
 
 typedef struct {
@@ -192,6 +192,250 @@ static PyTypeObject EntryType = {
     .tp_call = PyVectorcall_Call,
 };
 
+/* ---- calls around the BF16 and the 4-bit cache: these also check what they are given, before an address goes to a kernel --------
+ *
+ * How a C argument is formed from Python argument `arg`, and what is asked of it (all tensors on the context's device):
+ *   q, k rows [n][Hq or Hkv][d] in bfloat16, heads of a token contiguous; Q, K the same or None   s stride(0) of rows, 0 for None
+ *   e output rows [n][Hkv][d], o [n][Hq][d], bfloat16 or float32, contiguous     i [n] int32     t page table int32, two dimensions
+ *   l lengths int32, as many as the page table has rows    f float32 [Hq] or None      b, c pool of the BF16, of the 4-bit cache
+ *   h transform, an object with data_ptr(); H the same or None    w workspace    N n   0, 1, I, F, T, B, S as above (S of the device) */
+enum { QK_NORM_ROPE, BF16_APPEND, INT4_APPEND, INT4_GATHER, INT4_DECODE, N_OPERATORS };
+#define APPEND_PARAMS(pool) {{'H', 0}, {'k', 1}, {'s', 1}, {'k', 2}, {'s', 2}, {'i', 3}, {'i', 4}, {'N', 0}, {pool, 5}, {pool, 6}, {'0', 5}, {'t', 7}, {'1', 7}, {'0', 7}, \
+         {'l', 8}, {'Q', 9}, {'s', 9}, {'Q', 10}, {'s', 10}, {'S', 0}}
+/* rows: the argument that n is the first dimension of; table: the page table; pool: the pool of keys, the other follows it */
+static const struct { const char* name; int n_args, rows, table, pool; param p[MAX_ARGS]; } operators[N_OPERATORS] = {
+    /* transform, q, k, tok_pos, q_out, k_out */
+    [QK_NORM_ROPE] = {"novakv_qk_norm_rope", 6, 3, -1, -1,
+        {{'h', 0}, {'Q', 1}, {'s', 1}, {'K', 2}, {'s', 2}, {'i', 3}, {'N', 0}, {'Q', 4}, {'s', 4}, {'K', 5}, {'s', 5}, {'S', 0}}},
+    /* transform, k_new, v_new, tok_seq, tok_pos, k_pages, v_pages, page_table, seq_lens, q, q_out */
+    [BF16_APPEND] = {"novakv_bf16_append", 11, 1, 7, 5, APPEND_PARAMS('b')},
+    [INT4_APPEND] = {"novakv_int4_append", 11, 1, 7, 5, APPEND_PARAMS('c')},
+    /* tok_seq, tok_pos, k_pages, v_pages, page_table, k_out, v_out */
+    [INT4_GATHER] = {"novakv_int4_gather", 7, 0, 4, 2,
+        {{'i', 0}, {'i', 1}, {'N', 0}, {'c', 2}, {'c', 3}, {'0', 2}, {'t', 4}, {'1', 4}, {'0', 4}, {'e', 5}, {'e', 6}, {'T', 5}, {'S', 0}}},
+    /* q, k_pages, v_pages, page_table, seq_lens, out, workspace, sm_scale, window, sink_logits */
+    [INT4_DECODE] = {"novakv_int4_decode_attention", 10, 0, 3, 1,
+        {{'q', 0}, {'c', 1}, {'c', 2}, {'0', 1}, {'t', 3}, {'1', 3}, {'l', 4}, {'N', 0}, {'F', 7}, {'I', 8}, {'f', 9}, {'o', 5}, {'T', 5}, {'w', 6}, {'B', 6}, {'S', 0}}},
+};
+static PyObject *bfloat16, *int32, *uint8;                 /* of torch, given by bind_operators() */
+
+typedef struct {
+    PyObject_HEAD
+    vectorcallfunc vectorcall;
+    int entry;
+    void* fn;
+    long device, hq, hkv, d;
+    PyObject* py_device;
+} Operator;
+
+static int refuse(int op, int arg, const char* what) {
+    if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "%s: argument %d %s", operators[op].name, arg + 1, what);
+    return -1;
+}
+/* x.name() as an integer */
+static long method_int(PyObject* x, PyObject* name) {
+    PyObject* n = PyObject_CallMethodNoArgs(x, name);
+    if (!n) return -1;
+    const long v = n == Py_True ? 1 : n == Py_False ? 0 : PyLong_AsLong(n);
+    Py_DECREF(n);
+    return v;
+}
+/* sizes or strides of x into v; their number, or -1 */
+static int dims_of(PyObject* x, PyObject* name, int call, long long* v, int most) {
+    PyObject* s = call ? PyObject_CallMethodNoArgs(x, name) : PyObject_GetAttr(x, name);
+    if (!s) return -1;
+    int n = -1;
+    if (PyTuple_Check(s)) {
+        n = (int)PyTuple_GET_SIZE(s);
+        for (int i = 0; i < n && i < most; ++i) v[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(s, i));
+    }
+    Py_DECREF(s);
+    return n;
+}
+static int is_dtype(PyObject* x, PyObject* a, PyObject* b) {
+    PyObject* t = PyObject_GetAttr(x, s_dtype);
+    Py_XDECREF(t);
+    return t && (t == a || t == b);
+}
+/* what is asked of argument `arg`; n: rows of the call, table_rows, pool_pages of its page table and its first pool */
+static int check(const Operator* e, char kind, int arg, PyObject* x, long long n, long long table_rows, long long pool_pages) {
+    const int op = e->entry;
+    long long v[4] = {0, 0, 0, 0};
+    if (method_int(x, s_get_device) != e->device) return refuse(op, arg, "has to be a tensor on the context's device");
+    switch (kind) {
+        case 'q': case 'Q': case 'k': case 'K': {
+            const long heads = kind == 'q' || kind == 'Q' ? e->hq : e->hkv;
+            if (!is_dtype(x, bfloat16, bfloat16)) return refuse(op, arg, "has to be bfloat16");
+            if (dims_of(x, s_shape, 0, v, 4) != 3 || v[0] != n || v[1] != heads || v[2] != e->d) return refuse(op, arg, "has to be rows [n][heads][head_dim]");
+            if (dims_of(x, s_stride, 1, v, 4) != 3 || v[2] != 1 || (v[1] != e->d && heads > 1)) return refuse(op, arg, "has to have contiguous heads");
+            /* (decode attention takes no stride) */
+            if (kind == 'q' && n > 1 && v[0] != heads * e->d) return refuse(op, arg, "has to be contiguous");
+            return 0;
+        }
+        case 'e': case 'o':
+            if (!is_dtype(x, bfloat16, float32)) return refuse(op, arg, "has to be bfloat16 or float32");
+            if (dims_of(x, s_shape, 0, v, 4) != 3 || v[0] != n || v[1] != (kind == 'o' ? e->hq : e->hkv) || v[2] != e->d) return refuse(op, arg, "has to be rows [n][heads][head_dim]");
+            break;
+        case 'i':
+            if (!is_dtype(x, int32, int32) || dims_of(x, s_shape, 0, v, 4) != 1 || v[0] != n) return refuse(op, arg, "has to be int32, one for each row");
+            break;
+        case 't':
+            if (!is_dtype(x, int32, int32) || dims_of(x, s_shape, 0, v, 4) != 2) return refuse(op, arg, "has to be an int32 table [sequences][pages]");
+            break;
+        case 'l':
+            if (!is_dtype(x, int32, int32) || dims_of(x, s_shape, 0, v, 4) != 1 || v[0] != table_rows) return refuse(op, arg, "has to be int32, one for each row of the page table");
+            break;
+        case 'f':
+            if (!is_dtype(x, float32, float32) || dims_of(x, s_shape, 0, v, 4) != 1 || v[0] != e->hq) return refuse(op, arg, "has to be float32, one for each query head");
+            break;
+        case 'b': case 'c': {
+            long long bytes;
+            PyObject* b = PyObject_GetAttr(x, s_nbytes);
+            if (!b) return -1;
+            bytes = PyLong_AsLongLong(b);
+            Py_DECREF(b);
+            const long long row = kind == 'b' ? e->d * 2 : e->d / 2 + e->d / 64 * 4;
+            if (!is_dtype(x, kind == 'b' ? bfloat16 : uint8, NULL) || bytes != pool_pages * e->hkv * 64 * row || shape_of(x, 0) != pool_pages) return refuse(op, arg, "has to be a pool of this cache's pages, as many as the keys' pool");
+            break;
+        }
+        default: break;
+    }
+    if (method_int(x, s_is_contiguous) != 1) return refuse(op, arg, "has to be contiguous");
+    return 0;
+}
+
+static novakv_status call_operator(int entry, void* fn, novakv_ctx* c, const long long* a, float f) {
+#define I(i) ((int)a[i])
+#define V(i) ((void*)(uintptr_t)a[i])
+    switch (entry) {
+        case QK_NORM_ROPE:
+            return ((__typeof__(&novakv_qk_norm_rope))fn)(c, V(0), V(1), a[2], V(3), a[4], V(5), I(6), V(7), a[8], V(9), a[10], V(11));
+        case BF16_APPEND:
+        case INT4_APPEND:
+            return ((__typeof__(&novakv_int4_append))fn)(c, V(0), V(1), a[2], V(3), a[4], V(5), V(6), I(7), V(8), V(9), I(10), V(11), I(12), I(13), V(14), V(15), a[16],
+                                                         V(17), a[18], V(19));
+        case INT4_GATHER:
+            return ((__typeof__(&novakv_int4_gather))fn)(c, V(0), V(1), I(2), V(3), V(4), I(5), V(6), I(7), I(8), V(9), V(10), I(11), V(12));
+        default:
+            return ((__typeof__(&novakv_int4_decode_attention))fn)(c, V(0), V(1), V(2), I(3), V(4), I(5), V(6), I(7), f, I(9), V(10), V(11), I(12), V(13), (size_t)a[14], V(15));
+    }
+#undef I
+#undef V
+}
+
+/* operator(handle, arguments...) -> status */
+static PyObject* operator_call(PyObject* self, PyObject* const* args, size_t nargsf, PyObject* kwnames) {
+    const Operator* e = (const Operator*)self;
+    const int op = e->entry;
+    if (kwnames || PyVectorcall_NARGS(nargsf) != operators[op].n_args + 1) {
+        PyErr_Format(PyExc_TypeError, "%s: a context and %d positional arguments", operators[op].name, operators[op].n_args);
+        return NULL;
+    }
+    const unsigned long long ctx = args[0] == Py_None ? 0 : PyLong_AsUnsignedLongLong(args[0]);
+    if (PyErr_Occurred()) return NULL;
+    const long long n = shape_of(args[1 + operators[op].rows], 0);
+    if (PyErr_Occurred()) return NULL;
+    const long long table_rows = operators[op].table < 0 ? 0 : shape_of(args[1 + operators[op].table], 0);
+    if (PyErr_Occurred()) return NULL;
+    const long long pool_pages = operators[op].pool < 0 ? 0 : shape_of(args[1 + operators[op].pool], 0);
+    if (PyErr_Occurred()) return NULL;
+    if (op == INT4_DECODE && n != table_rows) { refuse(op, operators[op].table, "has to have one row for each query"); return NULL; }
+    if (n > 0x7fffffff || pool_pages > 0x7fffffff) { refuse(op, 0, "is too large"); return NULL; }
+    long long a[MAX_ARGS];
+    float f = 0.f;
+    const param* p = operators[op].p;
+    for (int i = 0; i < MAX_ARGS && p[i].kind; ++i) {
+        const int arg = p[i].arg;
+        PyObject* x = args[1 + arg];
+        unsigned long long u = 0;
+        long long v[4] = {0, 0, 0, 0};
+        a[i] = 0;
+        switch (p[i].kind) {
+            case 'Q': case 'K': case 'f':
+                if (x == Py_None) break;                   /* fall through */
+            case 'q': case 'k': case 'e': case 'o': case 'i': case 't': case 'l': case 'b': case 'c': case 'w':
+                if (x == Py_None) { refuse(op, arg, "is missing"); return NULL; }
+                if (check(e, p[i].kind, arg, x, n, table_rows, pool_pages) || pointer_of(x, &u)) return NULL;
+                a[i] = (long long)u;
+                break;
+            case 'h': case 'H':
+                if (x == Py_None && p[i].kind == 'h') { refuse(op, arg, "is missing"); return NULL; }
+                if (pointer_of(x, &u)) return NULL;
+                a[i] = (long long)u;
+                break;
+            case 's':
+                if (x == Py_None) break;
+                if (dims_of(x, s_stride, 1, v, 4) != 3) { refuse(op, arg, "has to be rows"); return NULL; }
+                a[i] = n > 1 ? v[0] : e->hq * e->d;        /* (of a single row any stride is one) */
+                break;
+            case 'N': a[i] = n; break;
+            case '0': a[i] = shape_of(x, 0); break;
+            case '1': a[i] = shape_of(x, 1); break;
+            case 'I': if (as_int(x, 0, &a[i])) return NULL; break;
+            case 'F': f = (float)PyFloat_AsDouble(x); break;
+            case 'T': a[i] = is_dtype(x, float32, float32); break;
+            case 'B': { PyObject* b = PyObject_GetAttr(x, s_nbytes); if (!b) return NULL; a[i] = PyLong_AsLongLong(b); Py_DECREF(b); break; }
+            default: {
+                PyObject* s = PyObject_CallOneArg(get_stream, e->py_device);
+                if (!s) return NULL;
+                a[i] = (long long)PyLong_AsUnsignedLongLong(s);
+                Py_DECREF(s);
+            }
+        }
+        if (PyErr_Occurred()) return NULL;
+    }
+    if (op == INT4_GATHER) {                               /* both outputs of one type */
+        if (is_dtype(args[6], float32, float32) != is_dtype(args[7], float32, float32)) { refuse(op, 6, "has to have the type of the keys' output"); return NULL; }
+    }
+    novakv_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = call_operator(op, e->fn, (novakv_ctx*)(uintptr_t)ctx, a, f);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
+static void operator_dealloc(PyObject* self) {
+    Py_XDECREF(((Operator*)self)->py_device);
+    PyObject_Free(self);
+}
+
+static PyTypeObject OperatorType = {
+    PyVarObject_HEAD_INIT(NULL, 0).tp_name = "_novakv_calls.Operator",
+    .tp_basicsize = sizeof(Operator),
+    .tp_flags = Py_TPFLAGS_DEFAULT | Py_TPFLAGS_HAVE_VECTORCALL,
+    .tp_vectorcall_offset = offsetof(Operator, vectorcall),
+    .tp_call = PyVectorcall_Call,
+    .tp_dealloc = operator_dealloc,
+};
+
+/* bind_operators(handle of the opened library, device, Hq, Hkv, head_dim, (torch.bfloat16, torch.int32, torch.uint8)) -> {name: operator} */
+static PyObject* bind_operators(PyObject* self, PyObject* args) {
+    PyObject *handle, *a, *b, *c;
+    long device, hq, hkv, d;
+    if (!PyArg_ParseTuple(args, "Ollll(OOO)", &handle, &device, &hq, &hkv, &d, &a, &b, &c)) return NULL;
+    void* h = PyLong_AsVoidPtr(handle);
+    if (PyErr_Occurred()) return NULL;
+    if (!get_stream) { PyErr_SetString(PyExc_RuntimeError, "setup() comes first"); return NULL; }
+    Py_INCREF(a); Py_INCREF(b); Py_INCREF(c);
+    Py_XSETREF(bfloat16, a);
+    Py_XSETREF(int32, b);
+    Py_XSETREF(uint8, c);
+    PyObject* dict = PyDict_New();
+    for (int i = 0; dict && i < N_OPERATORS; ++i) {
+        void* fn = dlsym(h, operators[i].name);
+        Operator* e = fn ? PyObject_New(Operator, &OperatorType) : NULL;
+        if (!fn) PyErr_Format(PyExc_RuntimeError, "the library lacks %s", operators[i].name);
+        if (e) {
+            e->vectorcall = operator_call; e->entry = i; e->fn = fn;
+            e->device = device; e->hq = hq; e->hkv = hkv; e->d = d;
+            e->py_device = PyLong_FromLong(device);
+        }
+        if (!e || !e->py_device || PyDict_SetItemString(dict, operators[i].name, (PyObject*)e)) Py_CLEAR(dict);
+        Py_XDECREF((PyObject*)e);
+    }
+    return dict;
+}
+
 /* setup(current stream of a device, current device, torch.float32): what the calls ask torch for */
 static PyObject* setup(PyObject* self, PyObject* args) {
     PyObject *a, *b, *c;
@@ -219,7 +463,8 @@ static PyObject* bind(PyObject* self, PyObject* handle) {
     return d;
 }
 
-static PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, NULL}, {"bind", bind, METH_O, NULL}, {NULL, NULL, 0, NULL}};
+static PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, NULL}, {"bind", bind, METH_O, NULL},
+                                {"bind_operators", bind_operators, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_novakv_calls", NULL, -1, methods};
 
 PyMODINIT_FUNC PyInit__novakv_calls(void) {
@@ -227,6 +472,10 @@ PyMODINIT_FUNC PyInit__novakv_calls(void) {
     s_shape = PyUnicode_InternFromString("shape");
     s_dtype = PyUnicode_InternFromString("dtype");
     s_nbytes = PyUnicode_InternFromString("nbytes");
-    if (!s_data_ptr || !s_shape || !s_dtype || !s_nbytes || PyType_Ready(&EntryType) < 0) return NULL;
+    s_stride = PyUnicode_InternFromString("stride");
+    s_get_device = PyUnicode_InternFromString("get_device");
+    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    if (!s_data_ptr || !s_shape || !s_dtype || !s_nbytes || !s_stride || !s_get_device || !s_is_contiguous || PyType_Ready(&EntryType) < 0 ||
+        PyType_Ready(&OperatorType) < 0) return NULL;
     return PyModule_Create(&module);
 }

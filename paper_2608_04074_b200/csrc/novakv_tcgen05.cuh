@@ -37,7 +37,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 }
 // Wait for an MMA that has been or will be issued by this CTA whatever happens: the flag does not end it.  (After a second
 // it raises the flag, after ten the MMA is given up for lost.)
-__device__ __noinline__ void mbar_wait_mma_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+static __device__ __noinline__ void mbar_wait_mma_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
     const long long t0 = clock64();
     for (;;) {
 #pragma unroll 1

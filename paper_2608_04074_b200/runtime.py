@@ -248,6 +248,76 @@ class BandedCache:
         return out
 
 
+class _RowCache:
+    """Page table, lengths and pools of a cache whose append takes the projection's rows (keys through a ``QKTransform``)."""
+
+    def __init__(self, ctx: Context, batch: int, capacity_tokens, seed: int = 0):
+        self.ctx, self.batch = ctx, batch
+        self.device = torch.device("cuda", ctx.cfg.device)
+        cap = np.maximum(np.broadcast_to(np.asarray(capacity_tokens, np.int32), (batch,)), 1)
+        table, n_pages = synth.shuffled_page_table(seed, cap, cache_format.PAGE_TOKENS)
+        self.n_pages, self.page_table_host = int(n_pages), table
+        self.page_table = torch.from_numpy(np.where(table < 0, 0, table).astype(np.int32)).to(self.device)
+        self.seq_lens = torch.zeros(batch, dtype=torch.int32, device=self.device)
+
+    def _q_out(self, q, q_out):
+        return torch.empty(q.shape, dtype=q.dtype, device=q.device) if q is not None and q_out is None else q_out
+
+    def _out(self, out):
+        return torch.empty((self.batch, self.ctx.n_q_heads, self.ctx.head_dim), dtype=torch.float32, device=self.device) if out is None else out
+
+
+class Int4Cache(_RowCache):
+    """Paged cache of 4-bit keys and values (one bf16 scale and zero per token, KV head and 64 channels): no calibration."""
+
+    def __init__(self, ctx: Context, batch: int, capacity_tokens, seed: int = 0):
+        super().__init__(ctx, batch, capacity_tokens, seed)
+        self.k_pages, self.v_pages = (torch.zeros((self.n_pages, ctx.novakv_int4_page_bytes()), dtype=torch.uint8, device=self.device)
+                                      for _ in range(2))
+        self.workspace = torch.empty(ctx.novakv_int4_workspace_bytes(batch), dtype=torch.uint8, device=self.device)
+
+    def append(self, transform, k_new, v_new, tok_seq, tok_pos, q=None, q_out=None):
+        """Keys and values of the listed tokens; with ``q`` also their queries through the transform, which are returned."""
+        q_out = self._q_out(q, q_out)
+        self.ctx.novakv_int4_append(transform, k_new, v_new, tok_seq, tok_pos, self.k_pages, self.v_pages, self.page_table,
+                                    self.seq_lens, q, q_out)
+        return q_out
+
+    def gather(self, tok_seq, tok_pos, dtype=torch.bfloat16):
+        k, v = (torch.empty((tok_seq.shape[0], self.ctx.n_kv_heads, self.ctx.head_dim), dtype=dtype, device=self.device) for _ in range(2))
+        self.ctx.novakv_int4_gather(tok_seq, tok_pos, self.k_pages, self.v_pages, self.page_table, k, v)
+        return k, v
+
+    def decode(self, q, out=None, sm_scale=None, window=0, sink_logits=None):
+        out = self._out(out)
+        self.ctx.novakv_int4_decode_attention(q, self.k_pages, self.v_pages, self.page_table, self.seq_lens, out, self.workspace,
+                                              sm_scale, window, sink_logits)
+        return out
+
+
+class BF16Cache(_RowCache):
+    """Paged cache of bf16 keys and values: the sliding-window layers."""
+
+    def __init__(self, ctx: Context, batch: int, capacity_tokens, seed: int = 0):
+        super().__init__(ctx, batch, capacity_tokens, seed)
+        shape = (self.n_pages, ctx.n_kv_heads, cache_format.PAGE_TOKENS, ctx.head_dim)
+        self.k_pages, self.v_pages = (torch.zeros(shape, dtype=torch.bfloat16, device=self.device) for _ in range(2))
+        self.workspace = torch.empty(ctx.novakv_bf16_workspace_bytes(batch, self.page_table.shape[1]), dtype=torch.uint8,
+                                     device=self.device)
+
+    def append(self, transform, k_new, v_new, tok_seq, tok_pos, q=None, q_out=None):
+        q_out = self._q_out(q, q_out)
+        self.ctx.novakv_bf16_append(transform, k_new, v_new, tok_seq, tok_pos, self.k_pages, self.v_pages, self.page_table,
+                                    self.seq_lens, q, q_out)
+        return q_out
+
+    def decode(self, q, out=None, sm_scale=None, window=0):
+        out = self._out(out)
+        self.ctx.novakv_bf16_decode_attention(q, self.k_pages, self.v_pages, self.page_table, self.seq_lens, out, self.workspace,
+                                              sm_scale, window)
+        return out
+
+
 def bf16_tensor(x: np.ndarray, device="cuda:0") -> torch.Tensor:
     """float array holding bf16-representable values -> torch bf16 tensor on the device."""
     return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(torch.bfloat16).to(device)
