@@ -386,7 +386,7 @@ novakv_status novakv_bf16_append(novakv_ctx* ctx, const novakv_qk_transform* tra
  * Keys and values as 4-bit integers with one bf16 (scale, zero) pair per token, KV head and 64 channels: 4.5 bits an element,
  * no calibration.  Of a group x_0 .. x_63 in binary32 (keys: the transformed key in binary64, rounded to binary32):
  *     zero  = bf16(min_i x_i)
- *     scale = bf16((max_i x_i - zero) / 15)     binary32; replaced by 1 if not positive and finite
+ *     scale = bf16((max_i x_i - zero) * fl(1/15))     binary32, fl(1/15) its nearest number; replaced by 1 if not positive and finite
  *     code_i = clamp(rint((x_i - zero) / scale), 0, 15)      binary32 subtraction and division, ties to even; NaN: 0
  *     read:  x^_i = zero + scale * code_i
  * A NaN in a group makes its zero, and so what is read of it, NaN.

@@ -13,9 +13,9 @@
 //  * Exactness: q is a bfloat16 number, exact in binary16 after a power of two per head; the weights are carried as binary16
 //    pairs hi + lo (22 bits).  With four heads the lo parts are the unused four columns of the same product; with eight they
 //    take a second one.  Accumulation, softmax statistics and the zeros' share are binary32.
-//  * Streaming: the walk over (sequence, KV head, tile of 32 tokens) is cut evenly among the CTAs (one per SM) and again among
-//    their 16 warps; each warp copies its tiles' keys and values (one bulk copy each) into a ring of its own, five tiles at
-//    d = 128, and no warp waits for another before the end.
+//  * Streaming: the walk over (sequence, KV head, unit of 32 or 64 tokens) is cut evenly among the CTAs (one per SM) and again among
+//    their 16 warps; each warp copies its units' keys and values (one bulk copy each) into a ring of its own, two units ahead,
+//    and no warp waits for another before the end.
 //  * Join: what a warp has of a (sequence, KV head) pair that it does not hold whole goes to shared memory; the CTA joins these
 //    pieces, and a second kernel joins the at most two per CTA that reach over its ends.
 #include <math_constants.h>
@@ -27,21 +27,30 @@
 namespace {
 
 constexpr int WARPS = 16, THREADS = WARPS * 32;
+constexpr int SLOTS = 2;                     // ring of a warp, in units (keys and values)
+// What setting up and writing out a (sequence, KV head) pair weighs in units, when the walk is cut.  32 sequences of 163 to 32768
+// tokens (d = 128, 8 KV heads): 57.4 us at 0, 52.4 at 1, 50.8 at 2, 49.6 at 3, 50.1 at 5; 8 x 16384 tokens 36.5 to 37 throughout.
+constexpr int PAIR_COST = 3;
 constexpr int HEADROOM = 4;                  // a new maximum is set this many bits high: the next records need no rescaling
 constexpr float W_ONE = 32768.f;             // the weight 1 in binary16: what underflows is 2^-39 of the largest
 
 template <int D, int HG>
 struct Plan {
     using Lay = I4Layout<D>;
-    static constexpr int SLOTS = D == 128 ? 5 : 10;                // ring of a warp, in tiles of one side
-    static constexpr int PIECE = HG * (D + 2);                     // floats of a partial: per head maximum, sum, accumulators
-    static constexpr int RING = WARPS * SLOTS * Lay::TILE_BYTES;
+    static constexpr int TILES = 128 / D;                          // tiles of a unit: what a warp copies, waits for and weighs at a time
+    static constexpr int TOKENS = TILES * I4_TILE;
+    static constexpr int HEAD = D + 4;                             // floats of a head's partial: maximum, sum, two unused, accumulators
+    static constexpr int PIECE = HG * HEAD;
+    static constexpr int SLOT = 2 * TILES * Lay::TILE_BYTES;
+    static constexpr int RING = WARPS * SLOTS * SLOT;
     static constexpr int BARS = RING;
-    static constexpr int HEADS = BARS + WARPS * SLOTS * 8;         // first pieces of the warps (the last ones lie in their rings)
-    static constexpr int PREFIX = HEADS + WARPS * PIECE * 4;       // int [THREADS + 1]
-    static constexpr int MISC = (PREFIX + (THREADS + 1) * 4 + 15) & ~15;
+    static constexpr int FRONT = BARS + WARPS * SLOTS * 8;         // first pieces of the warps (the last ones lie in their rings)
+    static constexpr int PREFIX = FRONT + WARPS * PIECE * 4;       // int [THREADS + 1]
+    static constexpr int SEQS = PREFIX + (THREADS + 1) * 4;        // int [THREADS + 1]
+    static constexpr int LENS = SEQS + (THREADS + 1) * 4;          // int [THREADS]
+    static constexpr int MISC = (LENS + THREADS * 4 + 15) & ~15;
     static constexpr int TOTAL = MISC + 512;
-    static_assert(SLOTS * Lay::TILE_BYTES >= PIECE * 4, "a warp's last piece fits into its ring");
+    static_assert(SLOTS * SLOT >= PIECE * 4, "a warp's last piece fits into its ring");
     static_assert(TOTAL <= 227 * 1024, "shared memory");
 };
 
@@ -50,7 +59,7 @@ struct DecodeArgs {
     const uint8_t *k_pages, *v_pages;
     int n_pages;
     const int32_t *page_table, *seq_lens;
-    int max_pages_per_seq, batch, hkv, window, out_is_fp32;
+    int max_pages_per_seq, batch, hkv, window, out_is_fp32, one;   // one: a CTA for each pair, which joins all of it
     float scale_log2;
     const float* sink;
     void* out;
@@ -101,64 +110,127 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     return __all_sync(0xffffffffu, mbar_wait_slow<0>(bar, parity, abort_flag));
 }
 
-// Sequence b's tiles in sight and its first one.
-struct Sight { int len, start, t0, tiles; };
-__device__ __forceinline__ Sight sight_of(const DecodeArgs& a, int b) {
+// Sequence b's units in sight and its first one.
+struct Sight { int len, start, t0, units; };
+template <int TOKENS>
+__device__ __forceinline__ Sight sight_of(const DecodeArgs& a, int len) {
     Sight s;
-    s.len = min(max(a.seq_lens[b], 0), a.max_pages_per_seq * NOVAKV_PAGE_TOKENS);
+    s.len = min(max(len, 0), a.max_pages_per_seq * NOVAKV_PAGE_TOKENS);
     s.start = a.window > 0 ? max(0, s.len - a.window) : 0;
-    s.t0 = s.start / I4_TILE;
-    s.tiles = s.len > 0 ? (s.len + I4_TILE - 1) / I4_TILE - s.t0 : 0;
+    s.t0 = s.start / TOKENS;
+    s.units = s.len > 0 ? (s.len + TOKENS - 1) / TOKENS - s.t0 : 0;
     return s;
 }
-// Where unit u of the walk lies: sequence, KV head, tile of the pair.
-struct Place { int b, kvh, tile; Sight s; };
-__device__ __forceinline__ Place locate(const DecodeArgs& a, const int* prefix, int chunk, long long u) {
-    int lo = 0, hi = THREADS;                                     // prefix[lo] hkv <= u < prefix[hi] hkv
+// Where a unit of the walk lies: sequence, KV head, unit of the pair.
+struct Place { int b, kvh, unit; Sight s; };
+// The walk over all pairs: prefix[i] units (of one KV head) and seqs[i] sequences with a token lie before sequence i chunk.
+struct Walk {
+    const int *prefix, *seqs, *lens;
+    int chunk;
+    __device__ __forceinline__ int len(const DecodeArgs& a, int b) const { return chunk == 1 ? lens[b] : a.seq_lens[b]; }
+    template <int TOKENS>
+    __device__ __forceinline__ Place place(const DecodeArgs& a, int i, long long u) const {     // u lies behind prefix[i], before prefix[i + 1]
+        Place p;
+        p.b = i * chunk;
+        long long r = u - (long long)prefix[i] * a.hkv;
+        p.s = sight_of<TOKENS>(a, len(a, p.b));
 #pragma unroll 1
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if ((long long)prefix[mid] * a.hkv <= u) lo = mid;
-        else hi = mid;
+        while (r >= (long long)p.s.units * a.hkv && p.b + 1 < a.batch) {
+            r -= (long long)p.s.units * a.hkv;
+            p.s = sight_of<TOKENS>(a, len(a, ++p.b));
+        }
+        const int units = max(p.s.units, 1);
+        p.kvh = min((int)r / units, a.hkv - 1);
+        p.unit = (int)r - p.kvh * units;
+        return p;
     }
-    Place p;
-    p.b = lo * chunk;
-    long long r = u - (long long)prefix[lo] * a.hkv;
-    p.s = sight_of(a, p.b);
+    // by one thread
+    template <int TOKENS>
+    __device__ __forceinline__ Place find(const DecodeArgs& a, long long u) const {
+        int lo = 0, hi = THREADS;                                 // prefix[lo] hkv <= u < prefix[hi] hkv
 #pragma unroll 1
-    while (r >= (long long)p.s.tiles * a.hkv && p.b + 1 < a.batch) {
-        r -= (long long)p.s.tiles * a.hkv;
-        p.s = sight_of(a, ++p.b);
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((long long)prefix[mid] * a.hkv <= u) lo = mid;
+            else hi = mid;
+        }
+        return place<TOKENS>(a, lo, u);
     }
-    const int tiles = max(p.s.tiles, 1);
-    p.kvh = min((int)r / tiles, a.hkv - 1);
-    p.tile = (int)r - p.kvh * tiles;
-    return p;
-}
+    // The walk is cut where the cost - units, and PAIR_COST for each pair - is even.  Units before cost x, by a warp.
+    __device__ __forceinline__ long long cost(const DecodeArgs& a, int i) const { return (prefix[i] + (long long)PAIR_COST * seqs[i]) * a.hkv; }
+    template <int TOKENS>
+    __device__ __forceinline__ long long units_before(const DecodeArgs& a, long long x, int lane) const {
+        constexpr int STEP = THREADS / 32;
+        int i = (31 - __clz(__ballot_sync(0xffffffffu, cost(a, lane * STEP) <= x))) * STEP;
+        i += 31 - __clz(__ballot_sync(0xffffffffu, lane < STEP && cost(a, i + lane % STEP) <= x));
+        long long left = x - cost(a, i), units = (long long)prefix[i] * a.hkv;
+        for (int b = i * chunk; b < min(a.batch, (i + 1) * chunk); ++b) {
+            const int n = sight_of<TOKENS>(a, len(a, b)).units;
+            if (n == 0) continue;
+            if (left < (long long)(n + PAIR_COST) * a.hkv) {
+                const int pair = (int)(left / (n + PAIR_COST));
+                return units + (long long)pair * n + max((int)(left - (long long)pair * (n + PAIR_COST)) - PAIR_COST, 0);
+            }
+            left -= (long long)(n + PAIR_COST) * a.hkv;
+            units += (long long)n * a.hkv;
+        }
+        return units;
+    }
+    // by a warp, for all of its lanes: 32 entries, then the 16 between two of them
+    template <int TOKENS>
+    __device__ __forceinline__ Place find_warp(const DecodeArgs& a, long long u, int lane) const {
+        constexpr int STEP = THREADS / 32;
+        const int i = 31 - __clz(__ballot_sync(0xffffffffu, (long long)prefix[lane * STEP] * a.hkv <= u));
+        const int k = 31 - __clz(__ballot_sync(0xffffffffu, lane < STEP && (long long)prefix[i * STEP + lane % STEP] * a.hkv <= u));
+        return place<TOKENS>(a, i * STEP + k, u);
+    }
+};
 
+// two neighbouring channels of the output [batch][Hkv][Hg][D], i counted from the pair's first
 template <int D, int HG>
-__device__ __forceinline__ void write_out(const DecodeArgs& a, int pair, int i, float o) {
-    const size_t oi = (size_t)pair * HG * D + i;                  // [batch][Hkv][Hg][D]
-    if (a.out_is_fp32) reinterpret_cast<float*>(a.out)[oi] = o;
-    else reinterpret_cast<__nv_bfloat16*>(a.out)[oi] = __float2bfloat16_rn(o);
+__device__ __forceinline__ void write_out2(const DecodeArgs& a, int pair, int i, float x, float y) {
+    const size_t oi = (size_t)pair * HG * D + i;
+    if (a.out_is_fp32) *reinterpret_cast<float2*>(reinterpret_cast<float*>(a.out) + oi) = make_float2(x, y);
+    else *reinterpret_cast<__nv_bfloat162*>(reinterpret_cast<__nv_bfloat16*>(a.out) + oi) = __floats2bfloat162_rn(x, y);
 }
 // the sink's share of a head's sum, relative to its maximum m
 __device__ __forceinline__ float sink_mass(const DecodeArgs& a, int head, float m) {
     return a.sink != nullptr ? ex2f(fmaf(a.sink[head], 1.44269504f, -m)) : 0.f;
 }
 
-template <int D, int HG>
+// Four codes of a word's 16-bit halves as binary16 numbers.  Plain: codes 0, 2 are c 2^-24, codes 1, 3 are 16 c 2^-24, five
+// instructions.  FINE: all four in the upper bits of the mantissa, c 2^-18, eight instructions: the tensor core aligns products by
+// the operands' exponents and cuts off what lies 2^-24 below, which for a subnormal number is counted from 2^-14 on, not from its
+// first bit, so that small ones lose up to ten of the product's bits.
+template <bool FINE>
+__device__ __forceinline__ void unpack_codes(uint32_t x, uint32_t (&c)[4]) {
+    if (FINE) {
+        c[0] = x << 6 & 0x03c003c0u; c[1] = x << 2 & 0x03c003c0u; c[2] = x >> 2 & 0x03c003c0u; c[3] = x >> 6 & 0x03c003c0u;
+    } else {
+        const uint32_t y = x >> 8;
+        c[0] = x & 0x000f000fu; c[1] = x & 0x00f000f0u; c[2] = y & 0x000f000fu; c[3] = y & 0x00f000f0u;
+    }
+}
+
+// FINE: for binary32 outputs.  The products keep the bits that they would lose (unpack_codes) and the weights meet the codes as
+// binary16 pairs hi + lo, in two products.  Without, a logit is off by less than 2^-11 of what one step of its key's largest
+// channel's code moves it by, and a weight by 2^-12 of itself, at random: an eighth of the rounding of a bfloat16 output.
+template <int D, int HG, bool FINE>
 __global__ void __launch_bounds__(THREADS, 1)
 novakv_int4_decode_kernel(const DecodeArgs a) {
     using Lay = I4Layout<D>;
     using P = Plan<D, HG>;
-    constexpr int G = Lay::GROUPS, NP = Lay::PIECES, SLOTS = P::SLOTS, TB = Lay::TILE_BYTES;
+    constexpr int G = Lay::GROUPS, NP = Lay::PIECES, TB = Lay::TILE_BYTES, UB = P::TILES * TB, S = P::TOKENS / 16;
+    // Columns of the products.  Eight heads fill the eight columns, and a lane holds two tokens of 16 for two heads.  With fewer
+    // heads columns 4..7 repeat columns 0..3, and the lanes that hold them take the other token: one token for two heads each.
+    constexpr bool SPLIT = HG < 8;
+    constexpr int R = SPLIT ? 1 : 2, COLS = SPLIT ? 4 : 8;
     extern __shared__ __align__(128) unsigned char smem[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, j = lane & 3;
-    int* prefix = reinterpret_cast<int*>(smem + P::PREFIX);
-    int* misc = reinterpret_cast<int*>(smem + P::MISC);           // 1 abort flag, 8..9 wait limit, 16..31 warp sums, 32..63 pieces' pairs, 64..95 their ends
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, j = lane & 3, up = SPLIT ? j >> 1 : 0, jj = SPLIT ? j & 1 : j;
+    int *prefix = reinterpret_cast<int*>(smem + P::PREFIX), *lens = reinterpret_cast<int*>(smem + P::LENS);
+    int* misc = reinterpret_cast<int*>(smem + P::MISC);           // 1 abort flag, 8..9 wait limit, 16..31 warp sums, 32..63 pieces' pairs, 64..95 their ends, 96..111 warp sums
     volatile int* abort_flag = misc + 1;
-    const uint32_t ring = smem_u32(smem) + warp * SLOTS * TB, bars = smem_u32(smem + P::BARS) + warp * SLOTS * 8;
+    const uint32_t ring = smem_u32(smem) + warp * SLOTS * P::SLOT, bars = smem_u32(smem + P::BARS) + warp * SLOTS * 8;
     if (lane < SLOTS) mbar_init(bars + 8 * lane, 1);
     if (threadIdx.x == 0) {
         misc[1] = 0;
@@ -168,106 +240,128 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     novakv_grid_dependency_wait();
 
-    // ---- the walk: prefix of the tiles by runs of `chunk` sequences -------------------------------------------------
-    const int chunk = (a.batch + THREADS - 1) / THREADS;
-    {
-        int sum = 0;
-        for (int b = threadIdx.x * chunk; b < min(a.batch, ((int)threadIdx.x + 1) * chunk); ++b) {
-            sum += sight_of(a, b).tiles;
-            if (blockIdx.x == 0 && a.seq_lens[b] > a.max_pages_per_seq * NOVAKV_PAGE_TOKENS) atomicOr(a.dev_status, NOVAKV_DEV_BAD_LENGTH);
+    // ---- the walk over (sequence, KV head, unit), and this warp's share of it
+    int* seqs = reinterpret_cast<int*>(smem + P::SEQS);
+    const Walk walk = {prefix, seqs, lens, (a.batch + THREADS - 1) / THREADS};
+    Place at = {};                                                // the warp's first unit
+    long long first = 0;
+    int n = 0;
+    bool idle = false;                                            // some sequence has no token
+    if (a.one) {
+        at.b = blockIdx.x / a.hkv;
+        at.kvh = blockIdx.x - at.b * a.hkv;
+        const int len = a.seq_lens[at.b];
+        at.s = sight_of<P::TOKENS>(a, len);
+        if (threadIdx.x == 0 && at.kvh == 0 && len > a.max_pages_per_seq * NOVAKV_PAGE_TOKENS) atomicOr(a.dev_status, NOVAKV_DEV_BAD_LENGTH);
+        at.unit = at.s.units * warp / WARPS;
+        n = at.s.units * (warp + 1) / WARPS - at.unit;
+        idle = at.s.units == 0;
+        __syncthreads();
+    } else {
+        int sum = 0, used = 0;
+        for (int b = threadIdx.x * walk.chunk; b < min(a.batch, ((int)threadIdx.x + 1) * walk.chunk); ++b) {
+            const int len = a.seq_lens[b], units = sight_of<P::TOKENS>(a, len).units;
+            sum += units;
+            used += units > 0;
+            if (walk.chunk == 1) lens[b] = len;
+            if (blockIdx.x == 0 && len > a.max_pages_per_seq * NOVAKV_PAGE_TOKENS) atomicOr(a.dev_status, NOVAKV_DEV_BAD_LENGTH);
+            idle |= units == 0;
         }
-        int inc = sum;
+        int inc = sum, inc_used = used;
 #pragma unroll
         for (int s = 1; s < 32; s <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, inc, s);
-            if (lane >= s) inc += o;
+            const int o = __shfl_up_sync(0xffffffffu, inc, s), u = __shfl_up_sync(0xffffffffu, inc_used, s);
+            if (lane >= s) { inc += o; inc_used += u; }
         }
-        if (lane == 31) misc[16 + warp] = inc;
+        if (lane == 31) { misc[16 + warp] = inc; misc[96 + warp] = inc_used; }
         __syncthreads();
-        int base = 0;
-        for (int w = 0; w < warp; ++w) base += misc[16 + w];
-        prefix[threadIdx.x + 1] = base + inc;
-        if (threadIdx.x == 0) prefix[0] = 0;
-        __syncthreads();
+        int base = lane < warp ? misc[16 + (lane & (WARPS - 1))] : 0, base_used = lane < warp ? misc[96 + (lane & (WARPS - 1))] : 0;
+#pragma unroll
+        for (int s = 1; s < WARPS; s <<= 1) {                     // (lanes from WARPS on hold 0)
+            base += __shfl_xor_sync(0xffffffffu, base, s);
+            base_used += __shfl_xor_sync(0xffffffffu, base_used, s);
+        }
+        prefix[threadIdx.x + 1] = __shfl_sync(0xffffffffu, base, 0) + inc;
+        seqs[threadIdx.x + 1] = __shfl_sync(0xffffffffu, base_used, 0) + inc_used;
+        if (threadIdx.x == 0) prefix[0] = seqs[0] = 0;
+        idle = __syncthreads_or(idle);
+        const long long total = walk.cost(a, THREADS);
+        // (no CTA in between without a unit, since the join goes by the CTAs' order: a CTA takes more cost than a pair's own)
+        const long long ctas = max(1ll, min((long long)gridDim.x, total / (PAIR_COST + 1))), cta = min((long long)blockIdx.x, ctas);
+        const long long c0 = total * cta / ctas, c1 = total * min(cta + 1, ctas) / ctas;
+        first = walk.units_before<P::TOKENS>(a, c0 + (c1 - c0) * warp / WARPS, lane);
+        n = (int)(walk.units_before<P::TOKENS>(a, c0 + (c1 - c0) * (warp + 1) / WARPS, lane) - first);
+        if (n > 0) at = walk.find_warp<P::TOKENS>(a, first, lane);
     }
-    const long long units = (long long)prefix[THREADS] * a.hkv;
-    // (no CTA in between without a unit: the join goes by the CTAs' order)
-    const long long ctas = max(1ll, min((long long)gridDim.x, units)), cta = min((long long)blockIdx.x, ctas);
-    const long long cu0 = units * cta / ctas, cu1 = units * min(cta + 1, ctas) / ctas;
-    const long long wu0 = cu0 + (cu1 - cu0) * warp / WARPS, wu1 = cu0 + (cu1 - cu0) * (warp + 1) / WARPS;
-    const int n = (int)(wu1 - wu0);
 
-    // ---- producer: the tiles' chunks 32 at a time, the next batch always on its way ---------------------------------
-    auto chunk_of = [&](int i) -> int {                           // (page, KV head, half) of the warp's i-th tile
+    // ---- producer: the units' chunks 32 at a time, the next batch always on its way
+    const Place begin = at;
+    auto chunk_of = [&](int i) -> int {                           // (page, KV head, part of the page) of the warp's i-th unit
         if (i >= n) return 0;
-        const Place p = locate(a, prefix, chunk, wu0 + i);
-        const int tile = p.s.t0 + p.tile;
-        int page = a.page_table[(size_t)p.b * a.max_pages_per_seq + tile / 2];
+        Place p = begin;
+        p.unit += i;
+        if (p.unit >= p.s.units) p = walk.find<P::TOKENS>(a, first + i);
+        const int unit = p.s.t0 + p.unit;
+        int page = a.page_table[(size_t)p.b * a.max_pages_per_seq + unit * P::TOKENS / NOVAKV_PAGE_TOKENS];
         if (page < 0 || page >= a.n_pages) {
             atomicOr(a.dev_status, NOVAKV_DEV_BAD_PAGE);
             page = 0;
         }
-        return (page * a.hkv + p.kvh) * 2 + (tile & 1);
+        return (page * a.hkv + p.kvh) * (NOVAKV_PAGE_TOKENS / P::TOKENS) + unit % (NOVAKV_PAGE_TOKENS / P::TOKENS);
     };
-    int batch_now = 0, chunks = 0, chunks_next = 0;
-    if (n > 0) { chunks = chunk_of(lane); if (n > 32) chunks_next = chunk_of(32 + lane); }
-    int put_slot = 0;
-    auto issue = [&](int item) {                                  // item 2 t: keys of tile t, 2 t + 1: its values
-        const int t = item >> 1;
-        if (t >> 5 != batch_now) {
-            batch_now = t >> 5;
+    int chunks = 0, chunks_next = 0;
+    auto issue = [&](int t) {                                     // unit t into slot t % SLOTS
+        if ((t & 31) == 0 && t > 0) {
             chunks = chunks_next;
-            chunks_next = chunk_of(((batch_now + 1) << 5) + lane);
+            chunks_next = chunk_of(t + 32 + lane);
         }
-        const size_t at = (size_t)__shfl_sync(0xffffffffu, chunks, t & 31) * TB;
+        const size_t at = (size_t)__shfl_sync(0xffffffffu, chunks, t & 31) * UB;
         if (lane == 0) {
-            mbar_expect_tx(bars + 8 * put_slot, TB);
-            bulk_copy(ring + put_slot * TB, ((item & 1) ? a.v_pages : a.k_pages) + at, TB, bars + 8 * put_slot);
+            const uint32_t bar = bars + 8 * (t % SLOTS), dst = ring + (t % SLOTS) * P::SLOT;
+            mbar_expect_tx(bar, 2 * UB);
+            bulk_copy(dst, a.k_pages + at, UB, bar);
+            bulk_copy(dst + UB, a.v_pages + at, UB, bar);
         }
-        put_slot = put_slot + 1 == SLOTS ? 0 : put_slot + 1;
     };
-    __syncwarp();
-    for (int i = 0; i < min(SLOTS, 2 * n); ++i) issue(i);
-    int issued = min(SLOTS, 2 * n), taken = 0, get_slot = 0, parity = 0;
-    bool given_up = false;
-    auto next_slot = [&]() {
-        if (++get_slot == SLOTS) { get_slot = 0; parity ^= 1; }
-        ++taken;
-    };
+    if (n > 0) {
+        chunks = chunk_of(lane);
+        __syncwarp();
+        for (int t = 0; t < min(SLOTS, n); ++t) issue(t);
+        if (n > 32) chunks_next = chunk_of(32 + lane);
+        __syncwarp();
+    }
 
     // ---- consumer ---------------------------------------------------------------------------------------------------
-    // the lane's columns 2 j, 2 j + 1 of the products: column c is head c % HG, its hi (c / HG = 0) or lo part (1)
-    const int head0 = 2 * j % HG, head1 = (2 * j + 1) % HG;
-    Place at = {};
-    if (n > 0) at = locate(a, prefix, chunk, wu0);
-    uint32_t qf[NP][2][2];
-    float qfac0 = 0.f, qfac1 = 0.f, qz0[G], qz1[G];
-    float m0, m1, l0, l1, zs0[G], zs1[G], vbound, vfac;
-    float o[NP][2][4];
-    bool fresh = true;
-    int seg_first = 0;
-
+    // the lane's columns 2 jj, 2 jj + 1: with fewer heads than columns some repeat, and are not looked at in the end
+    const int head0 = 2 * jj % HG, head1 = (2 * jj + 1) % HG;
+    // lane's row of the matrix loads: token lane % 16 (of 16), piece lane / 16 (of two)
+    const uint32_t mat = (lane & 15) * Lay::ROW + (((lane >> 4) ^ Lay::swizzle(lane & 15)) << 4);
+    const uint32_t pairs = Lay::pair(8 * up + gr, 0);
+    bool given_up = false;
+    int t = 0;
 #pragma unroll 1
-    for (int t = 0; t < n && !given_up; ++t) {
-        if (fresh) {                                              // ---- a new (sequence, KV head) pair
-            fresh = false;
-            seg_first = at.tile;
-            const __nv_bfloat16* qp = a.q + (((size_t)at.b * a.hkv + at.kvh) * HG + gr % HG) * D + 8 * j;
+    while (t < n && !given_up) {
+        // ---- a (sequence, KV head) pair: its queries as the products' columns
+        const int seg_first = at.unit, seg_n = min(at.s.units - at.unit, n - t);
+        uint32_t qf[NP][2][2];
+        float qfac, qz0[G], qz1[G];
+        {
+            const __nv_bfloat16* qp = a.q + (((size_t)at.b * a.hkv + at.kvh) * HG + gr % COLS % HG) * D + 8 * j;
             uint4 w[NP];
             float mx = 0.f;
 #pragma unroll
             for (int p = 0; p < NP; ++p) {
                 w[p] = *reinterpret_cast<const uint4*>(qp + 32 * p);
-                const uint32_t* ww = reinterpret_cast<const uint32_t*>(&w[p]);
+                const uint32_t ww[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(ww[i] << 16)), fabsf(__uint_as_float(ww[i] & 0xffff0000u))));
             }
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            // 2^up brings the head's largest coordinate just below 2^15
-            const int up = min(max(15 - ((int)(__float_as_uint(mx) >> 23) - 126), -100), 120);
-            const float f = __uint_as_float((uint32_t)(up + 127) << 23);
+#pragma unroll
+            for (int s = 1; s < 32; s <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
+            // 2^e brings the heads' largest coordinate just below 2^15 (what is 2^-31 of it or less loses bits)
+            const int e = min(max(15 - ((int)(__float_as_uint(mx) >> 23) - 126), -100), 120);
+            const float f = __uint_as_float((uint32_t)(e + 127) << 23), odd = FINE ? f : f * 0.0625f;
             float sum[G];
 #pragma unroll
             for (int g = 0; g < G; ++g) sum[g] = 0.f;
@@ -280,364 +374,437 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[p / 2] += x[i];
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {                     // channels 8 j + 2 s + {0, 4} in the low bits, + {1, 5} in bits 4..7
+                for (int s = 0; s < 2; ++s) {                     // codes 2 s, 2 s + 1 of a half: channels 8 j + 2 s + {0, 4}, + {1, 5}
                     qf[p][s][0] = pack_half(x[2 * s] * f, x[2 * s + 4] * f);
-                    qf[p][s][1] = pack_half(x[2 * s + 1] * f * 0.0625f, x[2 * s + 5] * f * 0.0625f);
+                    qf[p][s][1] = pack_half(x[2 * s + 1] * odd, x[2 * s + 5] * odd);
                 }
             }
-            const float fac = a.scale_log2 * __uint_as_float((uint32_t)(24 - up + 127) << 23);
-            qfac0 = __shfl_sync(0xffffffffu, fac, 8 * j);
-            qfac1 = __shfl_sync(0xffffffffu, fac, 8 * j + 4);
+            qfac = a.scale_log2 * __uint_as_float((uint32_t)((FINE ? 18 : 24) - e + 127) << 23);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 1);
                 sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 2);
-                qz0[g] = a.scale_log2 * __shfl_sync(0xffffffffu, sum[g], 8 * j);
-                qz1[g] = a.scale_log2 * __shfl_sync(0xffffffffu, sum[g], 8 * j + 4);
-                zs0[g] = zs1[g] = 0.f;
+                qz0[g] = a.scale_log2 * __shfl_sync(0xffffffffu, sum[g], 8 * jj);     // (lane 4 c holds column c)
+                qz1[g] = a.scale_log2 * __shfl_sync(0xffffffffu, sum[g], 8 * jj + 4);
             }
-            m0 = m1 = -CUDART_INF_F;
-            l0 = l1 = 0.f;
-            vbound = 0.f; vfac = 0.f;
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[p][s][i] = 0.f;
         }
-
-        // ---- logits of the tile's 32 tokens: z[s][0..1] of token 16 s + gr, z[s][2..3] of token 16 s + 8 + gr ---------
-        float z[2][4];
-        {
-            if (!warp_wait(bars + 8 * get_slot, parity, abort_flag)) { given_up = true; break; }
-            const uint32_t base = ring + get_slot * TB;
+        float m0 = -CUDART_INF_F, m1 = m0, l0 = 0.f, l1 = 0.f, zs0[G], zs1[G], vbound = 0.f, vfac = 0.f;
+        float o[NP][2][4];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
+        for (int g = 0; g < G; ++g) zs0[g] = zs1[g] = 0.f;
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[p][s][i] = 0.f;
+        // tokens in sight, counted from the unit's first one
+        int lo = at.s.start - (at.s.t0 + at.unit) * P::TOKENS, hi = at.s.len - (at.s.t0 + at.unit) * P::TOKENS;
+
+#pragma unroll 1
+        for (const int end = t + seg_n; t < end; ++t, lo -= P::TOKENS, hi -= P::TOKENS) {
+            const uint32_t kbase = ring + (t % SLOTS) * P::SLOT, vbase = kbase + UB;
+            if (!warp_wait(bars + 8 * (t % SLOTS), t / SLOTS & 1, abort_flag)) { given_up = true; break; }
+
+            // ---- logits: z[s][r] of token 16 s + 8 (SPLIT ? up : r) + gr
+            float z0[S][R], z1[S][R];
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
                 float acc[G][4];
 #pragma unroll
                 for (int g = 0; g < G; ++g)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[g][i] = 0.f;
-                const int row = 16 * s + (lane & 15);
 #pragma unroll
                 for (int pp = 0; pp < NP; pp += 2) {
                     uint32_t r[4];
-                    ldmatrix4(base + row * Lay::ROW + (((pp + (lane >> 4)) ^ Lay::swizzle(row)) << 4), r);
+                    ldmatrix4((kbase + mat ^ pp << 4) + s / 2 * TB + s % 2 * 16 * Lay::ROW, r);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const uint32_t x = r[2 * h], y = r[2 * h + 1];
-                        mma16816(acc[(pp + h) / 2], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[pp + h][0][0], qf[pp + h][0][1]);
-                        mma16816(acc[(pp + h) / 2], x >> 8 & 0x000f000fu, y >> 8 & 0x000f000fu, x >> 8 & 0x00f000f0u, y >> 8 & 0x00f000f0u,
-                                 qf[pp + h][1][0], qf[pp + h][1][1]);
+                        uint32_t x[4], y[4];
+                        unpack_codes<FINE>(r[2 * h], x);
+                        unpack_codes<FINE>(r[2 * h + 1], y);
+                        mma16816(acc[(pp + h) / 2], x[0], y[0], x[1], y[1], qf[pp + h][0][0], qf[pp + h][0][1]);
+                        mma16816(acc[(pp + h) / 2], x[2], y[2], x[3], y[3], qf[pp + h][1][0], qf[pp + h][1][1]);
                     }
                 }
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint32_t meta = base + Lay::pair(16 * s + 8 * half + gr, 0);
+                for (int r = 0; r < R; ++r) {
+                    const uint32_t meta = kbase + pairs + s / 2 * TB + (s % 2 * 16 + 8 * r) * G * 4;
                     uint32_t w[2];
                     if (G == 2) { const uint2 v = lds64(meta); w[0] = v.x; w[1] = v.y; }
                     else w[0] = w[1] = lds32(meta);
-                    float d0 = 0.f, d1 = 0.f, e0 = 0.f, e1 = 0.f;
+                    float d0 = 0.f, d1 = 0.f;
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        const float scale = __uint_as_float(w[g] << 16), zero = __uint_as_float(w[g] & 0xffff0000u);
-                        d0 = fmaf(scale, acc[g][2 * half], d0); d1 = fmaf(scale, acc[g][2 * half + 1], d1);
-                        e0 = fmaf(zero, qz0[g], e0); e1 = fmaf(zero, qz1[g], e1);
+                        const float scale = __uint_as_float(w[g] << 16) * qfac, zero = __uint_as_float(w[g] & 0xffff0000u);
+                        const float c0 = SPLIT ? (up ? acc[g][2] : acc[g][0]) : acc[g][2 * r], c1 = SPLIT ? (up ? acc[g][3] : acc[g][1]) : acc[g][2 * r + 1];
+                        d0 = fmaf(scale, c0, g ? fmaf(zero, qz0[g], d0) : zero * qz0[g]);
+                        d1 = fmaf(scale, c1, g ? fmaf(zero, qz1[g], d1) : zero * qz1[g]);
                     }
-                    z[s][2 * half] = fmaf(d0, qfac0, e0);
-                    z[s][2 * half + 1] = fmaf(d1, qfac1, e1);
+                    z0[s][r] = d0;
+                    z1[s][r] = d1;
                 }
             }
-            next_slot();
-            __syncwarp();
-            if (issued < 2 * n) { issue(issued); ++issued; }
-        }
 
-        // ---- scales and zeros of the values, tokens out of sight, running maximum --------------------------------------
-        if (!warp_wait(bars + 8 * get_slot, parity, abort_flag)) { given_up = true; break; }
-        const uint32_t vbase = ring + get_slot * TB;
-        float vs[2][2][G], vz[2][2][G];
+            // ---- scales and zeros of the values, tokens out of sight, running maximum
+            float vs[S][R][G], vz[S][R][G];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+            for (int s = 0; s < S; ++s)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const uint32_t meta = vbase + Lay::pair(16 * s + 8 * half + gr, 0);
-                uint32_t w[2];
-                if (G == 2) { const uint2 v = lds64(meta); w[0] = v.x; w[1] = v.y; }
-                else w[0] = w[1] = lds32(meta);
+                for (int r = 0; r < R; ++r) {
+                    const uint32_t meta = vbase + pairs + s / 2 * TB + (s % 2 * 16 + 8 * r) * G * 4;
+                    uint32_t w[2];
+                    if (G == 2) { const uint2 v = lds64(meta); w[0] = v.x; w[1] = v.y; }
+                    else w[0] = w[1] = lds32(meta);
 #pragma unroll
-                for (int g = 0; g < G; ++g) { vs[s][half][g] = __uint_as_float(w[g] << 16); vz[s][half][g] = __uint_as_float(w[g] & 0xffff0000u); }
-            }
-        const int tok0 = (at.s.t0 + at.tile) * I4_TILE;
-        if (tok0 < at.s.start || tok0 + I4_TILE > at.s.len) {     // (what lies out of sight is arbitrary bytes: nothing of it may count)
+                    for (int g = 0; g < G; ++g) { vs[s][r][g] = __uint_as_float(w[g] << 16); vz[s][r][g] = __uint_as_float(w[g] & 0xffff0000u); }
+                }
+            if (lo > 0 || hi < P::TOKENS) {                       // (what lies out of sight is arbitrary bytes: nothing of it may count)
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+                for (int s = 0; s < S; ++s)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int tok = tok0 + 16 * s + 8 * half + gr;
-                    if (tok < at.s.start || tok >= at.s.len) {
-                        z[s][2 * half] = z[s][2 * half + 1] = -CUDART_INF_F;
+                    for (int r = 0; r < R; ++r) {
+                        const int tok = 16 * s + 8 * (SPLIT ? up : r) + gr;
+                        if (tok < lo || tok >= hi) {
+                            z0[s][r] = z1[s][r] = -CUDART_INF_F;
 #pragma unroll
-                        for (int g = 0; g < G; ++g) vs[s][half][g] = vz[s][half][g] = 0.f;
+                            for (int g = 0; g < G; ++g) vs[s][r][g] = vz[s][r][g] = 0.f;
+                        }
                     }
-                }
-        }
-        {
-            const float x0 = fmaxf(fmaxf(z[0][0], z[0][2]), fmaxf(z[1][0], z[1][2])), x1 = fmaxf(fmaxf(z[0][1], z[0][3]), fmaxf(z[1][1], z[1][3]));
-            float vm = 0.f;
-#pragma unroll
-            for (int g = 0; g < G; ++g) vm = fmaxf(vm, fmaxf(fmaxf(vs[0][0][g], vs[0][1][g]), fmaxf(vs[1][0][g], vs[1][1][g])));
-            if (__any_sync(0xffffffffu, x0 > m0 || x1 > m1 || vm > vbound)) {
-                float y0 = x0, y1 = x1;
-#pragma unroll
-                for (int s = 4; s < 32; s <<= 1) {
-                    y0 = fmaxf(y0, __shfl_xor_sync(0xffffffffu, y0, s));
-                    y1 = fmaxf(y1, __shfl_xor_sync(0xffffffffu, y1, s));
-                    vm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, s));
-                }
-                const float n0 = y0 > m0 ? y0 + HEADROOM : m0, n1 = y1 > m1 ? y1 + HEADROOM : m1;
-                float a0 = n0 > m0 ? ex2f(m0 - n0) : 1.f, a1 = n1 > m1 ? ex2f(m1 - n1) : 1.f;
-                m0 = n0; m1 = n1;
-                l0 *= a0; l1 *= a1;
-#pragma unroll
-                for (int g = 0; g < G; ++g) { zs0[g] *= a0; zs1[g] *= a1; }
-                if (vm > vbound) {                                // power of two above the largest scale so far, with room
-                    const float nb = __uint_as_float(min(max((__float_as_uint(vm) >> 23) + 2u, 27u), 254u) << 23);
-                    const float r = vbound / nb;
-                    a0 *= r; a1 *= r;
-                    vbound = nb;
-                    vfac = W_ONE / nb;
-                }
-#pragma unroll
-                for (int p = 0; p < NP; ++p)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) { o[p][s][0] *= a0; o[p][s][1] *= a1; o[p][s][2] *= a0; o[p][s][3] *= a1; }
             }
-        }
-
-        // ---- weights and values --------------------------------------------------------------------------------------
+            {
+                float x0 = z0[0][0], x1 = z1[0][0], vm = 0.f;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            uint32_t b_hi[G][2], b_lo[G][2];
+                for (int s = 0; s < S; ++s)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const float p0 = ex2f(z[s][2 * half] - m0), p1 = ex2f(z[s][2 * half + 1] - m1);
-                l0 += p0; l1 += p1;
-                const float f0 = p0 * vfac, f1 = p1 * vfac;
+                    for (int r = 0; r < R; ++r) {
+                        x0 = fmaxf(x0, z0[s][r]);
+                        x1 = fmaxf(x1, z1[s][r]);
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    zs0[g] = fmaf(p0, vz[s][half][g], zs0[g]);
-                    zs1[g] = fmaf(p1, vz[s][half][g], zs1[g]);
-                    const float w0 = f0 * vs[s][half][g], w1 = f1 * vs[s][half][g];
-                    const uint32_t hi = pack_half(w0, w1);
-                    const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-                    const uint32_t lo = pack_half(w0 - back.x, w1 - back.y);
-                    if (HG == 8) {
-                        b_hi[g][half] = movmatrix_t(hi);
-                        b_lo[g][half] = movmatrix_t(lo);
-                    } else {
-                        const uint32_t mine = HG == 4 ? (j < 2 ? hi : lo) : HG == 2 ? (j == 0 ? hi : j == 1 ? lo : 0u) : (j == 0 ? (hi & 0xffffu) | (lo & 0xffff0000u) : 0u);
-                        b_hi[g][half] = movmatrix_t(mine);
+                        for (int g = 0; g < G; ++g) vm = fmaxf(vm, vs[s][r][g]);
                     }
-                }
-            }
-            const int row = 16 * s + (lane & 15);
+                if (__any_sync(0xffffffffu, x0 > m0 || x1 > m1 || vm > vbound)) {
 #pragma unroll
-            for (int pp = 0; pp < NP; pp += 2) {
-                uint32_t r[4];
-                ldmatrix4t(vbase + row * Lay::ROW + (((pp + (lane >> 4)) ^ Lay::swizzle(row)) << 4), r);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t x = r[2 * h], y = r[2 * h + 1];
-                    const int p = pp + h, g = p / 2;
-#pragma unroll
-                    for (int sh = 0; sh < 2; ++sh) {
-                        const uint32_t a0 = (sh ? x >> 8 : x) & 0x000f000fu, a1 = (sh ? x >> 8 : x) & 0x00f000f0u;
-                        const uint32_t a2 = (sh ? y >> 8 : y) & 0x000f000fu, a3 = (sh ? y >> 8 : y) & 0x00f000f0u;
-                        mma16816(o[p][sh], a0, a1, a2, a3, b_hi[g][0], b_hi[g][1]);
-                        if (HG == 8) mma16816(o[p][sh], a0, a1, a2, a3, b_lo[g][0], b_lo[g][1]);
+                    for (int s = SPLIT ? 2 : 4; s < 32; s <<= 1) {
+                        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, s));
+                        x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, s));
                     }
-                }
-            }
-        }
-        next_slot();
-        __syncwarp();
-        if (issued < 2 * n) { issue(issued); ++issued; }
-
-        // ---- end of the pair, or of the warp's share -------------------------------------------------------------------
-        const bool ends = at.tile + 1 == at.s.tiles;
-        if (ends || t + 1 == n) {
 #pragma unroll
-            for (int s = 4; s < 32; s <<= 1) {
-                l0 += __shfl_xor_sync(0xffffffffu, l0, s);
-                l1 += __shfl_xor_sync(0xffffffffu, l1, s);
+                    for (int s = 1; s < 32; s <<= 1) vm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, s));
+                    const float n0 = x0 > m0 ? x0 + HEADROOM : m0, n1 = x1 > m1 ? x1 + HEADROOM : m1;
+                    float a0 = n0 > m0 ? ex2f(m0 - n0) : 1.f, a1 = n1 > m1 ? ex2f(m1 - n1) : 1.f;
+                    m0 = n0; m1 = n1;
+                    l0 *= a0; l1 *= a1;
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    zs0[g] += __shfl_xor_sync(0xffffffffu, zs0[g], s);
-                    zs1[g] += __shfl_xor_sync(0xffffffffu, zs1[g], s);
-                }
-            }
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float v = o[p][s][i];
-                        if (HG == 4) v += __shfl_xor_sync(0xffffffffu, v, 2);
-                        if (HG == 2) v += __shfl_xor_sync(0xffffffffu, v, 1);
-                        o[p][s][i] = v * (16777216.f / W_ONE * (i < 2 ? 1.f : 0.0625f)) * vbound;
+                    for (int g = 0; g < G; ++g) { zs0[g] *= a0; zs1[g] *= a1; }
+                    if (vm > vbound) {                            // power of two above the largest scale so far, with room
+                        const float nb = __uint_as_float(min(max((__float_as_uint(vm) >> 23) + 2u, 27u), 254u) << 23);
+                        const float r = vbound / nb;
+                        a0 *= r; a1 *= r;
+                        vbound = nb;
+                        vfac = W_ONE / nb;
                     }
-            if (HG == 1)
-#pragma unroll
-                for (int p = 0; p < NP; ++p)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) { o[p][s][0] += o[p][s][1]; o[p][s][2] += o[p][s][3]; }
-            const int pair = at.b * a.hkv + at.kvh;
-            const bool whole = ends && seg_first == 0;
-            // the pieces of a warp that are not whole: one at its front, one at its back
-            const bool front = !whole && seg_first != 0;
-            float* dst = front ? reinterpret_cast<float*>(smem + P::HEADS) + warp * P::PIECE : reinterpret_cast<float*>(smem + warp * SLOTS * TB);
-            if (2 * j < (HG == 1 ? 2 : HG)) {                     // lane (gr, j): heads 2 j, 2 j + 1, channels 32 p + 4 gr + 0..3
-                float inv0 = 1.f, inv1 = 1.f;
-                if (whole) {
-                    inv0 = 1.f / (l0 + sink_mass(a, at.kvh * HG + head0, m0));
-                    inv1 = 1.f / (l1 + sink_mass(a, at.kvh * HG + head1, m1));
-                }
-#pragma unroll
-                for (int c = 0; c < (HG == 1 ? 1 : 2); ++c) {
-                    const int h = c ? head1 : head0;
-                    if (!whole && gr == 0) { dst[h * (D + 2)] = c ? m1 : m0; dst[h * (D + 2) + 1] = c ? l1 : l0; }
 #pragma unroll
                     for (int p = 0; p < NP; ++p)
 #pragma unroll
-                        for (int s = 0; s < 2; ++s)
-#pragma unroll
-                            for (int hf = 0; hf < 2; ++hf) {
-                                const int ch = 32 * p + 4 * gr + 2 * s + hf;
-                                const float v = o[p][s][2 * hf + c] + (c ? zs1[p / 2] : zs0[p / 2]);
-                                if (whole) write_out<D, HG>(a, pair, h * D + ch, v * (c ? inv1 : inv0));
-                                else dst[h * (D + 2) + 2 + ch] = v;
-                            }
+                        for (int s = 0; s < 2; ++s) { o[p][s][0] *= a0; o[p][s][1] *= a1; o[p][s][2] *= a0; o[p][s][3] *= a1; }
                 }
             }
-            if (!whole && lane == 0) {
-                misc[32 + 2 * warp + !front] = pair;
-                misc[64 + 2 * warp + !front] = (seg_first == 0) | ends << 1;
+
+            // ---- weights and values
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                uint32_t b_hi[G][2], b_lo[G][2];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float p0 = ex2f(z0[s][r] - m0), p1 = ex2f(z1[s][r] - m1);
+                    l0 += p0; l1 += p1;
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        zs0[g] = fmaf(p0, vz[s][r][g], zs0[g]);
+                        zs1[g] = fmaf(p1, vz[s][r][g], zs1[g]);
+                        const float f = vfac * vs[s][r][g], w0 = p0 * f, w1 = p1 * f;
+                        const uint32_t hi16 = pack_half(w0, w1), x = movmatrix_t(hi16);
+                        // SPLIT: columns 0..3 take the lower eight tokens, columns 4..7 the upper ones
+                        if (SPLIT) { b_hi[g][0] = gr < 4 ? x : 0u; b_hi[g][1] = gr < 4 ? 0u : x; }
+                        else b_hi[g][r] = x;
+                        if (FINE) {
+                            const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi16));
+                            const uint32_t y = movmatrix_t(pack_half(w0 - back.x, w1 - back.y));
+                            if (SPLIT) { b_lo[g][0] = gr < 4 ? y : 0u; b_lo[g][1] = gr < 4 ? 0u : y; }
+                            else b_lo[g][r] = y;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int pp = 0; pp < NP; pp += 2) {
+                    uint32_t r[4];
+                    ldmatrix4t((vbase + mat ^ pp << 4) + s / 2 * TB + s % 2 * 16 * Lay::ROW, r);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t x[4], y[4];
+                        const int p = pp + h, g = p / 2;
+                        unpack_codes<FINE>(r[2 * h], x);
+                        unpack_codes<FINE>(r[2 * h + 1], y);
+#pragma unroll
+                        for (int sh = 0; sh < 2; ++sh) {
+                            mma16816(o[p][sh], x[2 * sh], x[2 * sh + 1], y[2 * sh], y[2 * sh + 1], b_hi[g][0], b_hi[g][1]);
+                            if (FINE) mma16816(o[p][sh], x[2 * sh], x[2 * sh + 1], y[2 * sh], y[2 * sh + 1], b_lo[g][0], b_lo[g][1]);
+                        }
+                    }
+                }
             }
-            fresh = true;
+            __syncwarp();
+            if (t + SLOTS < n) issue(t + SLOTS);
         }
-        // ---- next tile
-        if (++at.tile == at.s.tiles) {
-            at.tile = 0;
-            if (++at.kvh == a.hkv && t + 1 < n) {
+        if (given_up) break;
+
+        // ---- end of the pair, or of the warp's share
+#pragma unroll
+        for (int s = SPLIT ? 2 : 4; s < 32; s <<= 1) {
+            l0 += __shfl_xor_sync(0xffffffffu, l0, s);
+            l1 += __shfl_xor_sync(0xffffffffu, l1, s);
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                zs0[g] += __shfl_xor_sync(0xffffffffu, zs0[g], s);
+                zs1[g] += __shfl_xor_sync(0xffffffffu, zs1[g], s);
+            }
+        }
+        const bool ends = seg_first + seg_n == at.s.units, whole = ends && seg_first == 0;
+        const int pair = at.b * a.hkv + at.kvh;
+        // the pieces of a warp that are not whole: one at its front (it does not begin its pair), one at its back
+        const bool front = seg_first != 0;
+        float* dst = reinterpret_cast<float*>(front ? smem + P::FRONT + warp * P::PIECE * 4 : smem + warp * SLOTS * P::SLOT);
+        float inv0 = 1.f, inv1 = 1.f;
+        if (whole) {
+            inv0 = 1.f / (l0 + sink_mass(a, at.kvh * HG + head0, m0));
+            inv1 = 1.f / (l1 + sink_mass(a, at.kvh * HG + head1, m1));
+        } else if (gr == 0 && up == 0) {
+            *reinterpret_cast<float2*>(dst + head0 * P::HEAD) = make_float2(m0, l0);
+            if (HG > 1) *reinterpret_cast<float2*>(dst + head1 * P::HEAD) = make_float2(m1, l1);
+        }
+        constexpr float UNIT = (FINE ? 262144.f : 16777216.f) / W_ONE;
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {                         // channels 32 p + 4 gr + 2 s, + 1 of the lane's two heads
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = o[p][s][i];
+                    if (SPLIT) v[i] += __shfl_xor_sync(0xffffffffu, v[i], 2);
+                    v[i] = fmaf(v[i] * (i < 2 || FINE ? UNIT : UNIT * 0.0625f), vbound, (i & 1) ? zs1[p / 2] : zs0[p / 2]);
+                }
+                if (2 * jj >= HG || (SPLIT && s != up)) continue; // (both halves hold the sums: each writes one s)
+                const int ch = 32 * p + 4 * gr + 2 * s;
+                if (whole) {
+                    write_out2<D, HG>(a, pair, head0 * D + ch, v[0] * inv0, v[2] * inv0);
+                    if (HG > 1) write_out2<D, HG>(a, pair, head1 * D + ch, v[1] * inv1, v[3] * inv1);
+                } else {
+                    *reinterpret_cast<float2*>(dst + head0 * P::HEAD + 4 + ch) = make_float2(v[0], v[2]);
+                    if (HG > 1) *reinterpret_cast<float2*>(dst + head1 * P::HEAD + 4 + ch) = make_float2(v[1], v[3]);
+                }
+            }
+        if (!whole && lane == 0) {
+            misc[32 + 2 * warp + !front] = pair;
+            misc[64 + 2 * warp + !front] = (seg_first == 0) | ends << 1;
+        }
+        // ---- next pair
+        if (t < n) {
+            at.unit = 0;
+            if (++at.kvh == a.hkv) {
                 at.kvh = 0;
-                do at.s = sight_of(a, ++at.b);
-                while (at.s.tiles == 0 && at.b + 1 < a.batch);
+                do at.s = sight_of<P::TOKENS>(a, walk.len(a, ++at.b));
+                while (at.s.units == 0 && at.b + 1 < a.batch);
             }
         }
     }
     if (given_up) {                                               // the copies in flight end before the shared memory does
-        for (; taken < issued; next_slot()) mbar_wait_mma(bars + 8 * get_slot, parity, abort_flag);
+        for (const int end = min(t + SLOTS, n); t < end; ++t) mbar_wait_mma(bars + 8 * (t % SLOTS), t / SLOTS & 1, abort_flag);
         if (lane == 0) atomicOr(a.dev_status, NOVAKV_DEV_WAIT_TIMEOUT);
     }
-    for (int b = blockIdx.x; b < a.batch; b += gridDim.x)         // sequences without a token
-        if (sight_of(a, b).tiles == 0)
-            for (int i = threadIdx.x; i < a.hkv * HG * D; i += THREADS) write_out<D, HG>(a, b * a.hkv, i, 0.f);
+    if (idle) {                                                   // sequences without a token
+        if (a.one) {
+            for (int i = 2 * threadIdx.x; i < HG * D; i += 2 * THREADS) write_out2<D, HG>(a, blockIdx.x, i, 0.f, 0.f);
+            return;
+        }
+        for (int b = blockIdx.x; b < a.batch; b += gridDim.x)
+            if (sight_of<P::TOKENS>(a, walk.len(a, b)).units == 0)
+                for (int i = 2 * threadIdx.x; i < a.hkv * HG * D; i += 2 * THREADS) write_out2<D, HG>(a, b * a.hkv, i, 0.f, 0.f);
+    }
 
-    // ---- join the warps' pieces --------------------------------------------------------------------------------------
+    // ---- join the warps' pieces: they lie in the order of the walk, those of a pair side by side; a warp takes a head of a pair
     __syncthreads();
-    int reach[2] = {-1, -1};
-    for (int i0 = 0; i0 < 2 * WARPS;) {
-        const int pair = misc[32 + i0];
-        if (pair < 0) { ++i0; continue; }
-        int i1 = i0, last = i0;
-        for (; i1 < 2 * WARPS && (misc[32 + i1] == pair || misc[32 + i1] < 0); ++i1)
-            if (misc[32 + i1] == pair) last = i1;
-        const bool begins = misc[64 + i0] & 1, ends = misc[64 + last] >> 1;
-        const int side = begins ? 1 : 0;
-        if (!(begins && ends)) reach[side] = pair;
-        float* to = a.part + ((size_t)blockIdx.x * 2 + side) * P::PIECE;
-        for (int i = threadIdx.x; i < HG * D; i += THREADS) {
-            const int h = i / D, c = i % D;
-            float m = -CUDART_INF_F;
-            for (int k = i0; k <= last; ++k)
-                if (misc[32 + k] == pair)
-                    m = fmaxf(m, ((k & 1) ? reinterpret_cast<const float*>(smem + (k >> 1) * SLOTS * TB) : reinterpret_cast<const float*>(smem + P::HEADS) + (k >> 1) * P::PIECE)[h * (D + 2)]);
-            float acc = 0.f, l = 0.f;
-            for (int k = i0; k <= last; ++k)
-                if (misc[32 + k] == pair) {
-                    const float* src = ((k & 1) ? reinterpret_cast<const float*>(smem + (k >> 1) * SLOTS * TB) : reinterpret_cast<const float*>(smem + P::HEADS) + (k >> 1) * P::PIECE) + h * (D + 2);
-                    const float f = src[0] == -CUDART_INF_F ? 0.f : ex2f(src[0] - m);
-                    acc = fmaf(f, src[2 + c], acc);
-                    l = fmaf(f, src[1], l);
-                }
+    const int mine = misc[32 + lane], ends_of = mine >= 0 ? misc[64 + lane] : 0;
+    const uint32_t valid = __ballot_sync(0xffffffffu, mine >= 0), below = valid & ((1u << lane) - 1);
+    const int before = __shfl_sync(0xffffffffu, mine, below ? 31 - __clz(below) : 0);
+    uint32_t starts = __ballot_sync(0xffffffffu, mine >= 0 && (below == 0 || before != mine));
+    int reach_front = -1, reach_back = -1, task = 0;
+    while (starts) {
+        const int first = __ffs(starts) - 1, pair = __shfl_sync(0xffffffffu, mine, first);
+        starts &= starts - 1;
+        const uint32_t pieces = __ballot_sync(0xffffffffu, mine == pair);
+        const bool begins = __shfl_sync(0xffffffffu, ends_of, first) & 1, ends = __shfl_sync(0xffffffffu, ends_of, 31 - __clz(pieces)) >> 1;
+        if (!begins) reach_front = pair;
+        else if (!ends) reach_back = pair;
+        for (int h = 0; h < HG; ++h) {
+            if ((task++ & (WARPS - 1)) != warp) continue;
+            auto piece = [&](int k) { return reinterpret_cast<const float*>(k & 1 ? smem + (k >> 1) * SLOTS * P::SLOT : smem + P::FRONT + (k >> 1) * P::PIECE * 4) + h * P::HEAD; };
+            const float2 ml = mine == pair ? *reinterpret_cast<const float2*>(piece(lane)) : make_float2(-CUDART_INF_F, 0.f);
+            float m = ml.x;
+#pragma unroll
+            for (int s = 1; s < 32; s <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+            const float f = ml.x == -CUDART_INF_F ? 0.f : ex2f(ml.x - m);
+            float l = f * ml.y;
+#pragma unroll
+            for (int s = 1; s < 32; s <<= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+            float acc[D / 32];
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) acc[i] = 0.f;
+            for (uint32_t left = pieces; left; left &= left - 1) {
+                const int k = __ffs(left) - 1;
+                const float fk = __shfl_sync(0xffffffffu, f, k);
+                const float* src = piece(k) + 4 + lane * (D / 32);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) acc[i] = fmaf(fk, src[i], acc[i]);
+            }
             if (begins && ends) {
-                write_out<D, HG>(a, pair, i, acc / (l + sink_mass(a, pair % a.hkv * HG + h, m)));
+                const float inv = 1.f / (l + sink_mass(a, pair % a.hkv * HG + h, m));
+#pragma unroll
+                for (int i = 0; i < D / 32; i += 2) write_out2<D, HG>(a, pair, h * D + lane * (D / 32) + i, acc[i] * inv, acc[i + 1] * inv);
             } else {
-                to[h * (D + 2) + 2 + c] = acc;
-                if (c == 0) { to[h * (D + 2)] = m; to[h * (D + 2) + 1] = l; }
+                float* to = a.part + ((size_t)blockIdx.x * 2 + begins) * P::PIECE + h * P::HEAD;
+                if (lane == 0) *reinterpret_cast<float2*>(to) = make_float2(m, l);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) to[4 + lane * (D / 32) + i] = acc[i];
             }
         }
-        i0 = last + 1;
     }
-    if (threadIdx.x < 2) a.info[2 * blockIdx.x + threadIdx.x] = threadIdx.x ? reach[1] : reach[0];
+    if (!a.one && threadIdx.x < 2) a.info[2 * blockIdx.x + threadIdx.x] = threadIdx.x ? reach_back : reach_front;
 }
 
-// One block per CTA of the scan: joins the pair that begins in it and reaches over its back end, with the front pieces of the
-// CTAs behind it.
-constexpr int MERGE_THREADS = 512;
+// One block per CTA of the scan: joins the pair that begins in the CTA and reaches over its back end with the front pieces of the
+// CTAs behind it.  A warp takes a head and every GROUPS-th piece; what it loads hangs on two loads in a row, the pairs' numbers
+// and the pieces (a chain of four took 4.5 us of a decode step of one sequence of 16384 tokens, this MERGE_US).
+constexpr int MERGE_WARPS = 16;
 template <int D, int HG>
-__global__ void __launch_bounds__(MERGE_THREADS)
+__global__ void __launch_bounds__(MERGE_WARPS * 32)
 novakv_int4_merge_kernel(const DecodeArgs a) {
-    constexpr int PIECE = Plan<D, HG>::PIECE;
+    using P = Plan<D, HG>;
+    constexpr int N = D / 32, GROUPS = MERGE_WARPS / HG, BATCH = 4;
+    __shared__ float s_ml[MERGE_WARPS][2], s_acc[MERGE_WARPS][D];
     novakv_grid_dependency_wait();
-    const int c0 = blockIdx.x, pair = a.info[2 * c0 + 1];
+    const int c0 = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x & 31, h = warp % HG, g = warp / HG, left = gridDim.x - c0;
+    const int pair = a.info[2 * c0 + 1], behind = lane > 0 && lane < left ? a.info[2 * (c0 + lane)] : -1;
     if (pair < 0) return;
-    const int parts = 1 + __syncthreads_count(c0 + 1 + threadIdx.x < gridDim.x && a.info[2 * (c0 + 1 + threadIdx.x)] == pair);
-    for (int i = threadIdx.x; i < HG * D; i += MERGE_THREADS) {
-        const int h = i / D, c = i % D;
-        float m = -CUDART_INF_F;
-        for (int k = 0; k < parts; ++k) m = fmaxf(m, a.part[((size_t)(c0 + k) * 2 + (k == 0)) * PIECE + h * (D + 2)]);
-        float acc = 0.f, l = 0.f;
-        for (int k = 0; k < parts; ++k) {
-            const float* src = a.part + ((size_t)(c0 + k) * 2 + (k == 0)) * PIECE + h * (D + 2);
-            const float f = src[0] == -CUDART_INF_F ? 0.f : ex2f(src[0] - m);
-            acc = fmaf(f, src[2 + c], acc);
-            l = fmaf(f, src[1], l);
+    // pieces lie side by side: k = 0 is the back piece of this CTA, k > 0 the front piece of CTA c0 + k
+    int parts = __popc(__ballot_sync(0xffffffffu, lane == 0 || behind == pair));
+    for (int k0 = 32; parts == k0; k0 += 32) parts += __popc(__ballot_sync(0xffffffffu, k0 + lane < left && a.info[2 * (c0 + k0 + lane)] == pair));
+    float m = -CUDART_INF_F, l = 0.f, acc[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) acc[i] = 0.f;
+    for (int k0 = g; k0 < parts; k0 += BATCH * GROUPS) {
+        float2 ml[BATCH];
+        float v[BATCH][N];
+#pragma unroll
+        for (int e = 0; e < BATCH; ++e) {
+            const int k = min(k0 + e * GROUPS, parts - 1);
+            const float* src = a.part + ((size_t)(c0 + k) * 2 + (k == 0)) * P::PIECE + h * P::HEAD;
+            ml[e] = *reinterpret_cast<const float2*>(src);
+#pragma unroll
+            for (int i = 0; i < N; i += 2) {
+                const float2 x = *reinterpret_cast<const float2*>(src + 4 + lane * N + i);
+                v[e][i] = x.x; v[e][i + 1] = x.y;
+            }
         }
-        write_out<D, HG>(a, pair, i, acc / (l + sink_mass(a, pair % a.hkv * HG + h, m)));
+        float mx = m;
+#pragma unroll
+        for (int e = 0; e < BATCH; ++e) {
+            if (k0 + e * GROUPS >= parts) ml[e] = make_float2(-CUDART_INF_F, 0.f);
+            mx = fmaxf(mx, ml[e].x);
+        }
+        const float old = m == -CUDART_INF_F ? 0.f : ex2f(m - mx);
+        m = mx;
+        l *= old;
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] *= old;
+#pragma unroll
+        for (int e = 0; e < BATCH; ++e) {
+            const float f = ml[e].x == -CUDART_INF_F ? 0.f : ex2f(ml[e].x - m);
+            l = fmaf(f, ml[e].y, l);
+#pragma unroll
+            for (int i = 0; i < N; ++i) acc[i] = k0 + e * GROUPS < parts ? fmaf(f, v[e][i], acc[i]) : acc[i];
+        }
     }
+    if (GROUPS > 1) {
+        if (lane == 0) { s_ml[warp][0] = m; s_ml[warp][1] = l; }
+#pragma unroll
+        for (int i = 0; i < N; ++i) s_acc[warp][lane * N + i] = acc[i];
+        __syncthreads();
+        if (g > 0) return;
+        float mx = m;
+#pragma unroll
+        for (int e = 1; e < GROUPS; ++e) mx = fmaxf(mx, s_ml[e * HG + h][0]);
+        const float old = m == -CUDART_INF_F ? 0.f : ex2f(m - mx);
+        m = mx;
+        l *= old;
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] *= old;
+#pragma unroll
+        for (int e = 1; e < GROUPS; ++e) {
+            const float me = s_ml[e * HG + h][0], f = me == -CUDART_INF_F ? 0.f : ex2f(me - m);
+            l = fmaf(f, s_ml[e * HG + h][1], l);
+#pragma unroll
+            for (int i = 0; i < N; ++i) acc[i] = fmaf(f, s_acc[e * HG + h][lane * N + i], acc[i]);
+        }
+    }
+    const float inv = 1.f / (l + sink_mass(a, pair % a.hkv * HG + h, m));
+#pragma unroll
+    for (int i = 0; i < N; i += 2) write_out2<D, HG>(a, pair, h * D + lane * N + i, acc[i] * inv, acc[i + 1] * inv);
 }
 
+// Units of a warp up to which a CTA keeps a pair to itself.  One sequence, 8 pairs, one CTA each / split over all and joined:
+// d = 128, 777 tokens (2 units a warp) 8.6 / 11.7 us, 1500 (3) 10.7 / 11.9, 2048 (4) 12.4 / 12.8, 4096 (8) 18.6 / 12.4;
+// d = 64, 700 tokens (1) 6.0 / 9.6, 2000 (2) 8.8 / 10.7, 4000 (4) 12.3 / 11.6.
+constexpr int ONE_UNITS = 3;
 int scan_ctas(const novakv_ctx* ctx) { return ctx->scan_ctas > 0 && ctx->scan_ctas < ctx->n_sm ? ctx->scan_ctas : ctx->n_sm; }
 size_t info_bytes(const novakv_ctx* ctx) { return ((size_t)ctx->n_sm * 2 * sizeof(int) + 255) & ~(size_t)255; }
 
-template <int D, int HG>
-novakv_status launch(novakv_ctx* ctx, DecodeArgs& a, void* workspace, cudaStream_t stream) {
+template <int D, int HG, bool FINE>
+novakv_status launch_t(novakv_ctx* ctx, DecodeArgs& a, void* workspace, cudaStream_t stream) {
     using P = Plan<D, HG>;
-    auto* kern = novakv_int4_decode_kernel<D, HG>;
-    const unsigned bit = 1u << (__builtin_ctz(HG) + (D == 128 ? 4 : 0));
+    auto* kern = novakv_int4_decode_kernel<D, HG, FINE>;
+    const unsigned bit = 1u << (__builtin_ctz(HG) + (D == 128 ? 4 : 0) + (FINE ? 8 : 0));
     if (!(ctx->int4_opt_in & bit)) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, P::TOTAL) != cudaSuccess) return NOVAKV_ECUDA;
         ctx->int4_opt_in |= bit;
     }
     a.info = (int*)workspace;
     a.part = (float*)((char*)workspace + info_bytes(ctx));
-    const dim3 grid(scan_ctas(ctx));
+    // One CTA for each pair, and no second kernel, where every pair has an SM to itself and its warps few units each.
+    const long long pairs = (long long)a.batch * a.hkv;
+    const int seen = a.window > 0 ? min(a.window / P::TOKENS + 2, a.max_pages_per_seq * (NOVAKV_PAGE_TOKENS / P::TOKENS))
+                                  : a.max_pages_per_seq * (NOVAKV_PAGE_TOKENS / P::TOKENS);
+    a.one = pairs <= scan_ctas(ctx) && seen <= ONE_UNITS * WARPS;
+    const dim3 grid(a.one ? (int)pairs : scan_ctas(ctx));
     if (novakv_launch_pdl(kern, grid, dim3(THREADS), P::TOTAL, stream, a) != cudaSuccess) return NOVAKV_ECUDA;
     ctx->launches++;
-    if (novakv_launch_pdl(novakv_int4_merge_kernel<D, HG>, grid, dim3(MERGE_THREADS), 0, stream, a) != cudaSuccess) return NOVAKV_ECUDA;
+    if (a.one) return NOVAKV_OK;
+    if (novakv_launch_pdl(novakv_int4_merge_kernel<D, HG>, grid, dim3(MERGE_WARPS * 32), 0, stream, a) != cudaSuccess) return NOVAKV_ECUDA;
     ctx->launches++;
     return NOVAKV_OK;
+}
+template <int D, int HG>
+novakv_status launch(novakv_ctx* ctx, DecodeArgs& a, void* workspace, cudaStream_t stream) {
+    return a.out_is_fp32 ? launch_t<D, HG, true>(ctx, a, workspace, stream) : launch_t<D, HG, false>(ctx, a, workspace, stream);
 }
 
 }  // namespace
 
 extern "C" size_t novakv_int4_workspace_bytes(const novakv_ctx* ctx, int batch) {
     if (!ctx || batch <= 0) return 0;
-    return info_bytes(ctx) + (size_t)ctx->n_sm * 2 * ctx->hg * (ctx->cfg.head_dim + 2) * sizeof(float);
+    return info_bytes(ctx) + (size_t)ctx->n_sm * 2 * ctx->hg * (ctx->cfg.head_dim + 4) * sizeof(float);
 }
 
 extern "C" novakv_status novakv_int4_decode_attention(novakv_ctx* ctx, const void* q, const uint8_t* k_pages, const uint8_t* v_pages,
@@ -649,7 +816,7 @@ extern "C" novakv_status novakv_int4_decode_attention(novakv_ctx* ctx, const voi
     if (n_pages <= 0 || max_pages_per_seq <= 0) return NOVAKV_EPAGE;
     if (((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages) & 15) return NOVAKV_EINVAL;
     if (((uintptr_t)page_table | (uintptr_t)seq_lens | (uintptr_t)sink_logits) & 3) return NOVAKV_EINVAL;
-    if ((uintptr_t)out & (out_is_fp32 ? 3 : 1)) return NOVAKV_EINVAL;
+    if ((uintptr_t)out & (out_is_fp32 ? 7 : 3)) return NOVAKV_EINVAL;
     if (!(sm_scale == sm_scale)) return NOVAKV_EINVAL;
     const long long hkv = ctx->cfg.n_kv_heads;
     // (tiles of the pools and of the batch are counted in 32 bits)

@@ -3,12 +3,13 @@
 //
 //     y = x rsqrt(mean_i x_i^2 + eps) w                      per head, where a weight is given
 //     (a, b) -> A (a cos t - b sin t, b cos t + a sin t)     t = position * inv_freq, in binary64
-//     4 bits: zero = bf16(min), scale = bf16((max - zero) / 15), code = clamp(rint((x - zero) / scale), 0, 15) per 64 channels
+//     4 bits: zero = bf16(min), scale = bf16((max - zero) * (1/15)), code = clamp(rint((x - zero) / scale), 0, 15) per 64 channels
 //
 // Every call moves each element once, so it is bound by memory where it is long and by latency where it is short.  A row (one
 // head of one token) belongs to D / 16 lanes with two units of 8 channels each (two 16-byte loads); with rotation by halves the
-// two units are a unit and its partner, so that no value crosses lanes but in the sums and minima.  A block takes a few tokens
-// with all of their heads, q, k and v: the angles are formed once for them, while the first rows are on their way.
+// two units are a unit and its partner, so that no value crosses lanes but in the sums and minima.  A warp takes the rows of one
+// token (few tokens: several warps a part of them each): every row of a lane then meets the same eight angles, which stay in
+// registers, and nothing waits for another warp.
 #include <math_constants.h>
 
 #include "novakv_int4.cuh"
@@ -16,7 +17,7 @@
 
 namespace {
 
-constexpr int ROT_THREADS = 256;
+constexpr int ROT_THREADS = 128;
 enum { DST_ROWS, DST_BF16, DST_INT4 };       // k goes to rows, to the BF16 pool, to the 4-bit pool
 
 struct RotateArgs {
@@ -24,22 +25,17 @@ struct RotateArgs {
     long long q_stride, k_stride, v_stride, q_out_stride, k_out_stride;    // elements from token to token
     __nv_bfloat16 *q_out, *k_out;
     const int32_t *tok_seq, *tok_pos;
-    int n_tokens, hq, hkv, tokens_per_block;
+    int n_tokens, hq, hkv, parts;            // parts: warps of a token
     const float* inv_freq;
     const __nv_bfloat16 *q_weight, *k_weight;
     float eps, amplitude;
-    int rot_dim, interleaved;
+    int rot_dim;
     uint8_t *k_pages, *v_pages;              // (the BF16 pools too)
     int n_pages, max_pages_per_seq, n_seq;
     const int32_t* page_table;
     int32_t* seq_lens;
     uint32_t* dev_status;
 };
-
-// The key of the 4-bit cache is formed in binary64: the definition's codes and bfloat16 pairs are those of the exact number
-// rounded to binary32, and a key formed in binary32 would now and then fall to the other side of a border.
-__device__ __forceinline__ float rsqrt_of(float mean, float eps) { return rsqrtf(mean + eps); }
-__device__ __forceinline__ double rsqrt_of(double mean, float eps) { return 1.0 / sqrt(mean + (double)eps); }
 
 template <bool VEC>
 __device__ __forceinline__ uint4 load_unit(const __nv_bfloat16* p) {
@@ -82,208 +78,363 @@ __device__ __forceinline__ uint4 pack_unit(const T (&x)[8]) {
 __device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 
-// norm and rotation of a row's two units; cs: (cos, sin) of the token's angles.  All lanes of the warp take part.
-template <int D, typename T, typename T2>
-__device__ __forceinline__ void transform_row(const RotateArgs& a, const __nv_bfloat16* weight, const T2* cs, int ua, int ub, T (&x)[8], T (&y)[8]) {
+// What a lane knows of its token and layer: (cos, sin) of its eight pairs - (x_i, y_i), or neighbours (IL) x_2i, x_2i+1 for i < 4
+// and y_2i-8, y_2i-7 - and its channels' weights.
+struct Turn {
+    float c[8], s[8];
+};
+// the angle of a lane's pair i
+template <bool IL>
+__device__ __forceinline__ int angle_of(int i, int ua, int ub) { return !IL ? 8 * ua + i : i < 4 ? 4 * ua + i : 4 * ub + i - 4; }
+template <bool IL>
+__device__ __forceinline__ float& first_of(int i, float (&x)[8], float (&y)[8]) { return !IL ? x[i] : i < 4 ? x[2 * i] : y[2 * i - 8]; }
+template <bool IL>
+__device__ __forceinline__ float& second_of(int i, float (&x)[8], float (&y)[8]) { return !IL ? y[i] : i < 4 ? x[2 * i + 1] : y[2 * i - 7]; }
+
+// norm (wx, wy: the units' weights) and rotation of a row's two units.  All lanes of the warp take part.  False where the sum of
+// squares leaves the range in which its roundings are relative ones.
+template <int D, bool IL>
+__device__ __forceinline__ bool transform_row(const RotateArgs& a, bool norm, const uint4& wx, const uint4& wy, const Turn& turn, float (&x)[8], float (&y)[8]) {
     constexpr int LANES = D / 16;
-    if (weight != nullptr) {
-        T ss = 0;
+    bool fine = true;
+    if (norm) {
+        float ss = 0.f, st = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { ss += x[i] * x[i]; ss += y[i] * y[i]; }
+        for (int i = 0; i < 8; ++i) { ss = fmaf(x[i], x[i], ss); st = fmaf(y[i], y[i], st); }
+        ss += st;
 #pragma unroll
         for (int s = 1; s < LANES; s <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
-        const T r = rsqrt_of(ss / D, a.eps);
+        const float r = rsqrtf(fmaf(ss, 1.f / D, a.eps));
+        fine = ss > 1e-30f && ss < 1e30f;
+        float w[8];
+        unpack_unit(wx, w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[i] = x[i] * r * (T)__bfloat162float(weight[8 * ua + i]);
-            y[i] = y[i] * r * (T)__bfloat162float(weight[8 * ub + i]);
-        }
+        for (int i = 0; i < 8; ++i) x[i] *= r * w[i];
+        unpack_unit(wy, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] *= r * w[i];
     }
-    if (8 * ua >= a.rot_dim) return;                              // (without rotation rot_dim is 0)
-    if (!a.interleaved) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const T2 c = cs[8 * ua + i];
-            const T u = x[i] * c.x - y[i] * c.y;
-            y[i] = y[i] * c.x + x[i] * c.y;
-            x[i] = u;
-        }
-    } else {
+    for (int i = 0; i < 8; ++i) {                                 // (a pair that is not rotated has the angle 0)
+        float &p = first_of<IL>(i, x, y), &q = second_of<IL>(i, x, y);
+        const float u = p * turn.c[i] - q * turn.s[i];
+        q = q * turn.c[i] + p * turn.s[i];
+        p = u;
+    }
+    return fine;
+}
+
+// Quotients by one scale.  With r the nearest number to 1 / s and q0 = x r, q0 + (x - q0 s) r with fused multiply-adds is the
+// nearest number to x / s (P. Markstein, 1990) while nothing overflows or underflows; groups out of that range are divided.
+struct Divisor {
+    float s, r;
+    __device__ __forceinline__ explicit Divisor(float scale) : s(scale), r(1.f / scale) {}
+    __device__ __forceinline__ float quotient(float x) const {
+        const float q0 = x * r;
+        return fmaf(fmaf(-q0, s, x), r, q0);
+    }
+};
+constexpr float ROUND = 12582912.f;          // 1.5 2^23: added and taken away again it leaves the nearest integer, ties to even
+
+// Codes and pairs of a row.  All lanes of the warp take part.
+// A value row is given exactly.  A key (KEY) is defined by binary64, but formed in binary32 first: each element is off by less
+// than 2^-19 (|a| + |b|) of the pair it comes from (a mean of D squares, a root, the weight, cos and sin, two products and a sum:
+// 29 roundings of 2^-24), which is at most sqrt(2) times that of the pair it gives.  Where no element, minimum or maximum can
+// have crossed a border of its rounding by that, codes and pairs are those of the binary64 key; else the answer is false, and
+// the row is formed again in binary64: some 3 % of the warps' rows.
+template <int D, bool KEY>
+struct Quantised {
+    uint32_t wx, wy;
+    float zero[I4Layout<D>::GROUPS], scale[I4Layout<D>::GROUPS];
+
+    template <bool INTERLEAVED>
+    __device__ __forceinline__ bool form(int ua, int ub, const float (&x)[8], const float (&y)[8]) {
+        constexpr int G = I4Layout<D>::GROUPS, LANES = D / 16;
+        constexpr float OFF = 2.75e-6f;                           // sqrt(2) 2^-19 = 2.70e-6
+        bool sure = true, ranged = true;
+        float dx[8], dy[8];
+        float xl = x[0], xh = x[0], yl = y[0], yh = y[0], xl2, xh2, yl2, yh2;
+        if (KEY) {
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            T2 c = cs[4 * ua + i / 2];
-            T u = x[i] * c.x - x[i + 1] * c.y;
-            x[i + 1] = x[i + 1] * c.x + x[i] * c.y;
-            x[i] = u;
-            if (8 * ub < a.rot_dim) {
-                c = cs[4 * ub + i / 2];
-                u = y[i] * c.x - y[i + 1] * c.y;
-                y[i + 1] = y[i + 1] * c.x + y[i] * c.y;
-                y[i] = u;
+            for (int i = 0; i < 8; ++i) {
+                dx[i] = OFF * (fabsf(x[i]) + fabsf(INTERLEAVED ? x[i ^ 1] : y[i]));
+                dy[i] = INTERLEAVED ? OFF * (fabsf(y[i]) + fabsf(y[i ^ 1])) : dx[i];
             }
+            // upper ends in xl, xh, yl, yh, lower ends in the others; of the lower ends fmin passes a NaN over, the upper keep it
+            xl = xh = x[0] + dx[0]; yl = yh = y[0] + dy[0];
+            xl2 = xh2 = x[0] - dx[0]; yl2 = yh2 = y[0] - dy[0];
         }
-    }
-}
-
-__device__ __forceinline__ uint32_t code_word(const float (&x)[8], float zero, float scale) {
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)                                   // (a NaN gets code 0)
-        w |= (uint32_t)__float2int_rn(fminf(fmaxf(__fdiv_rn(x[i] - zero, scale), 0.f), 15.f)) << (4 * i);
-    return w;
-}
-
-// a row into the 4-bit chunk of its (page, KV head).  All lanes of the warp take part; `live` ones write.
-template <int D>
-__device__ __forceinline__ void store_row4(uint8_t* chunk, int slot, int l, int ua, int ub, const float (&x)[8], const float (&y)[8], bool live) {
-    using Lay = I4Layout<D>;
-    constexpr int LANES = D / 16;
-    float lo[Lay::GROUPS], hi[Lay::GROUPS];
-    {
-        float xl = x[0], xh = x[0], yl = y[0], yh = y[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) {
-            xl = min_nan(xl, x[i]); xh = max_nan(xh, x[i]);
-            yl = min_nan(yl, y[i]); yh = max_nan(yh, y[i]);
-        }
-#pragma unroll
-        for (int g = 0; g < Lay::GROUPS; ++g) {
-            const bool xin = Lay::GROUPS == 1 || ua / 8 == g, yin = Lay::GROUPS == 1 || ub / 8 == g;
-            lo[g] = min_nan(xin ? xl : CUDART_INF_F, yin ? yl : CUDART_INF_F);
-            hi[g] = max_nan(xin ? xh : -CUDART_INF_F, yin ? yh : -CUDART_INF_F);
-#pragma unroll
-            for (int s = 1; s < LANES; s <<= 1) {
-                lo[g] = min_nan(lo[g], __shfl_xor_sync(0xffffffffu, lo[g], s));
-                hi[g] = max_nan(hi[g], __shfl_xor_sync(0xffffffffu, hi[g], s));
+            const float u = KEY ? x[i] + dx[i] : x[i], v = KEY ? y[i] + dy[i] : y[i];
+            xl = min_nan(xl, u); xh = max_nan(xh, u);
+            yl = min_nan(yl, v); yh = max_nan(yh, v);
+            if (KEY) {
+                xl2 = fminf(xl2, x[i] - dx[i]); yl2 = fminf(yl2, y[i] - dy[i]);
+                xh2 = fmaxf(xh2, x[i] - dx[i]); yh2 = fmaxf(yh2, y[i] - dy[i]);
             }
         }
-    }
-    if (!live) return;
-    float zero[Lay::GROUPS], scale[Lay::GROUPS];
 #pragma unroll
-    for (int g = 0; g < Lay::GROUPS; ++g) {
-        zero[g] = __bfloat162float(__float2bfloat16_rn(lo[g]));
-        scale[g] = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(hi[g] - zero[g], 15.f)));
-        if (!(scale[g] > 0.f && scale[g] < CUDART_INF_F)) scale[g] = 1.f;
-    }
-    const int ga = Lay::GROUPS == 1 ? 0 : ua / 8, gb = Lay::GROUPS == 1 ? 0 : ub / 8;
-    uint8_t* tile = chunk + (slot / I4_TILE) * Lay::TILE_BYTES;
-    const int t = slot % I4_TILE;
-    *reinterpret_cast<uint32_t*>(tile + Lay::word(t, ua)) = code_word(x, ga ? zero[Lay::GROUPS - 1] : zero[0], ga ? scale[Lay::GROUPS - 1] : scale[0]);
-    *reinterpret_cast<uint32_t*>(tile + Lay::word(t, ub)) = code_word(y, gb ? zero[Lay::GROUPS - 1] : zero[0], gb ? scale[Lay::GROUPS - 1] : scale[0]);
-    if (l < Lay::GROUPS)                                          // (both numbers are bfloat16: the upper half of their bits)
-        *reinterpret_cast<uint32_t*>(tile + Lay::pair(t, l)) =
-            __float_as_uint(l ? scale[Lay::GROUPS - 1] : scale[0]) >> 16 | (__float_as_uint(l ? zero[Lay::GROUPS - 1] : zero[0]) & 0xffff0000u);
-}
-
-template <int D, int DST, bool VEC>
-__global__ void __launch_bounds__(ROT_THREADS)
-novakv_rotate_kernel(const RotateArgs a) {
-    constexpr int LANES = D / 16, RPW = 32 / LANES, WARPS = ROT_THREADS / 32;
-    extern __shared__ __align__(16) unsigned char smem[];
-    const int tpb = a.tokens_per_block, half = a.rot_dim / 2;
-    float2* cs = reinterpret_cast<float2*>(smem);                 // [tokens][half]
-    double2* cd = reinterpret_cast<double2*>(smem + (((size_t)tpb * half * 8 + 15) & ~(size_t)15));
-    int2* where = reinterpret_cast<int2*>(smem + (((size_t)tpb * half * 8 + 15) & ~(size_t)15) + (DST == DST_INT4 ? (size_t)tpb * half * 16 : 0));
-    novakv_grid_dependency_wait();
-    const int tok0 = blockIdx.x * tpb, n_tok = min(tpb, a.n_tokens - tok0);
-    for (int i = threadIdx.x; i < n_tok * half; i += ROT_THREADS) {
-        const int t = i / half, f = i - t * half;
-        const double angle = (double)a.tok_pos[tok0 + t] * (double)a.inv_freq[f];
-        if (DST == DST_INT4) {
-            double s, c;
-            sincos(angle, &s, &c);
-            c *= (double)a.amplitude; s *= (double)a.amplitude;
-            cd[i] = make_double2(c, s);
-            cs[i] = make_float2((float)c, (float)s);
-        } else {
-            // turns in binary64 (a far position keeps its angle), what is left of them in binary32
-            double turns = angle * 0.15915494309189533577;
-            turns -= rint(turns);
-            float s, c;
-            sincospif(2.f * (float)turns, &s, &c);
-            cs[i] = make_float2(c * a.amplitude, s * a.amplitude);
-        }
-    }
-    if (DST != DST_ROWS) {                                        // slot of every token: (page, slot), page -1: skipped
-        for (int t = threadIdx.x; t < n_tok; t += ROT_THREADS) {
-            const int seq = a.tok_seq[tok0 + t], pos = a.tok_pos[tok0 + t];
-            int page = -1;
-            if (seq != -1) {
-                if (seq < 0 || seq >= a.n_seq || pos < 0 || pos / NOVAKV_PAGE_TOKENS >= a.max_pages_per_seq) {
-                    atomicOr(a.dev_status, NOVAKV_DEV_BAD_TOKEN);
-                } else {
-                    page = a.page_table[(size_t)seq * a.max_pages_per_seq + pos / NOVAKV_PAGE_TOKENS];
-                    if (page < 0 || page >= a.n_pages) {
-                        atomicOr(a.dev_status, NOVAKV_DEV_BAD_PAGE);
-                        page = -1;
-                    } else if (a.seq_lens[seq] <= pos) {          // (lengths only grow: a stale one costs an atomic)
-                        atomicMax(&a.seq_lens[seq], pos + 1);
-                    }
+        for (int g = 0; g < G; ++g) {
+            const bool xin = G == 1 || ua / 8 == g, yin = G == 1 || ub / 8 == g;
+            float lo = min_nan(xin ? xl : CUDART_INF_F, yin ? yl : CUDART_INF_F), hi = max_nan(xin ? xh : -CUDART_INF_F, yin ? yh : -CUDART_INF_F);
+            if (!KEY) {
+#pragma unroll
+                for (int s = 1; s < LANES; s <<= 1) {
+                    lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, s));
+                    hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, s));
                 }
+                zero[g] = __bfloat162float(__float2bfloat16_rn(lo));
+                scale[g] = scale_of(hi, zero[g]);
+                ranged = ranged && zero[g] > -1e28f && hi < 1e28f && scale[g] > 1e-28f;
+            } else {
+                const float lo2 = fminf(xin ? xl2 : CUDART_INF_F, yin ? yl2 : CUDART_INF_F);
+                float hi2 = fmaxf(xin ? xh2 : -CUDART_INF_F, yin ? yh2 : -CUDART_INF_F);
+                __nv_bfloat162 both = __floats2bfloat162_rn(lo, lo2);   // (rounding keeps the order)
+#pragma unroll
+                for (int s = 1; s < LANES; s <<= 1) {
+                    const uint32_t o = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t*>(&both), s);
+                    both = __hmin2_nan(both, *reinterpret_cast<const __nv_bfloat162*>(&o));
+                    hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, s));
+                    hi2 = fmaxf(hi2, __shfl_xor_sync(0xffffffffu, hi2, s));
+                }
+                zero[g] = __low2float(both);
+                scale[g] = scale_of(hi, zero[g]);
+                sure = sure && zero[g] == __high2float(both) && scale[g] == scale_of(hi2, zero[g]) && scale[g] > 1e-28f && zero[g] > -1e28f && hi < 1e28f;
             }
-            where[t] = make_int2(page, pos % NOVAKV_PAGE_TOKENS);
+        }
+        const int ga = G == 1 ? 0 : ua / 8, gb = G == 1 ? 0 : ub / 8;
+        const float zx = ga ? zero[G - 1] : zero[0], zy = gb ? zero[G - 1] : zero[0];
+        const Divisor qx(ga ? scale[G - 1] : scale[0]), qy(gb ? scale[G - 1] : scale[0]);
+        float worst = 0.f;                                        // of the distances from the codes, errors included
+        wx = unit(x, dx, zx, qx, worst);
+        wy = unit(y, dy, zy, qy, worst);
+        if (!KEY && !ranged) {
+            wx = unit_divided(x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7], zx, qx.s);
+            wy = unit_divided(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7], zy, qy.s);
+        }
+        // (difference and quotient themselves are off by 2e-6 at most, here and where they are defined)
+        return sure && worst < 0.499992f;
+    }
+    // the code word of a unit: two times four codes as a number of 16 bits
+    static __device__ __forceinline__ uint32_t unit(const float (&x)[8], const float (&d)[8], float zero, const Divisor& by, float& worst) {
+        float half[2];
+#pragma unroll
+        for (int i = 7; i >= 0; --i) {
+            const float t = fminf(fmaxf(by.quotient(x[i] - zero), 0.f), 15.f);        // (a NaN gets code 0)
+            const float c = __fadd_rn(__fadd_rn(t, ROUND), -ROUND);
+            if (KEY) worst = fmaxf(worst, fmaf(d[i], by.r, fabsf(t - c)));
+            half[i / 4] = i % 4 == 3 ? c : fmaf(half[i / 4], 16.f, c);
+        }
+        return __byte_perm(__float_as_uint(half[0] + 8388608.f), __float_as_uint(half[1] + 8388608.f), 0x5410);
+    }
+    static __device__ __noinline__ uint32_t unit_divided(float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7, float zero, float scale) {
+        const float x[8] = {x0, x1, x2, x3, x4, x5, x6, x7};
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w |= (uint32_t)__float2int_rn(fminf(fmaxf(__fdiv_rn(x[i] - zero, scale), 0.f), 15.f)) << (4 * i);
+        return w;
+    }
+    static __device__ __forceinline__ float scale_of(float hi, float zero) {
+        const float s = __bfloat162float(__float2bfloat16_rn(__fmul_rn(hi - zero, 1.f / 15.f)));
+        return s > 0.f && s < CUDART_INF_F ? s : 1.f;
+    }
+    __device__ __forceinline__ void store(uint8_t* chunk, int slot, int l, int ua, int ub) const {
+        using Lay = I4Layout<D>;
+        uint8_t* tile = chunk + (slot / I4_TILE) * Lay::TILE_BYTES;
+        const int t = slot % I4_TILE;
+        *reinterpret_cast<uint32_t*>(tile + Lay::word(t, ua)) = wx;
+        *reinterpret_cast<uint32_t*>(tile + Lay::word(t, ub)) = wy;
+        if (l < Lay::GROUPS)                                      // (both numbers are bfloat16: the upper half of their bits)
+            *reinterpret_cast<uint32_t*>(tile + Lay::pair(t, l)) =
+                __float_as_uint(l ? scale[Lay::GROUPS - 1] : scale[0]) >> 16 | (__float_as_uint(l ? zero[Lay::GROUPS - 1] : zero[0]) & 0xffff0000u);
+    }
+};
+
+// A key row in binary64, from the row as it was given, to its slot: what its codes are defined by.  (A call, and by value: the
+// rows of the binary32 path stay in registers.)
+template <int D, bool IL>
+__device__ __noinline__ void store_row64(const RotateArgs& a, int pos, int l, int ua, int ub, uint4 ra, uint4 rb, uint8_t* chunk, bool live) {
+    constexpr int LANES = D / 16;
+    float xo[8], yo[8];
+    double x[8], y[8];
+    unpack_unit(ra, xo);
+    unpack_unit(rb, yo);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { x[i] = xo[i]; y[i] = yo[i]; }
+    if (a.k_weight != nullptr) {
+        double ss = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss += x[i] * x[i] + y[i] * y[i];
+#pragma unroll
+        for (int s = 1; s < LANES; s <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
+        const double r = 1.0 / sqrt(ss / D + (double)a.eps);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] *= r * (double)__bfloat162float(a.k_weight[8 * ua + i]);
+            y[i] *= r * (double)__bfloat162float(a.k_weight[8 * ub + i]);
         }
     }
-    __syncthreads();
+    const double amp = a.amplitude;
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+        const int f = angle_of<IL>(i, ua, ub);
+        if (8 * (IL && i >= 4 ? ub : ua) >= a.rot_dim) continue;
+        double s, c;
+        sincos((double)pos * (double)a.inv_freq[f], &s, &c);
+        double &p = !IL ? x[i] : i < 4 ? x[2 * i] : y[2 * i - 8], &q = !IL ? y[i] : i < 4 ? x[2 * i + 1] : y[2 * i - 7];
+        const double v = amp * (p * c - q * s);
+        q = amp * (q * c + p * s);
+        p = v;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { xo[i] = (float)x[i]; yo[i] = (float)y[i]; }
+    Quantised<D, false> code;
+    code.template form<false>(ua, ub, xo, yo);
+    if (live) code.store(chunk, pos % NOVAKV_PAGE_TOKENS, l, ua, ub);
+}
 
+template <int D, int DST, bool VEC, bool IL>
+__global__ void __launch_bounds__(ROT_THREADS, DST == DST_INT4 ? 5 : 7)
+novakv_rotate_kernel(const __grid_constant__ RotateArgs a) {
+    constexpr int LANES = D / 16, RPW = 32 / LANES, WARPS = ROT_THREADS / 32;
     const int lane = threadIdx.x & 31, sub = lane / LANES, l = lane % LANES;
-    const int wq = (n_tok * a.hq + RPW - 1) / RPW, wk = (n_tok * a.hkv + RPW - 1) / RPW;
-    const int tasks = wq + wk + (DST == DST_ROWS ? 0 : wk);
+    const int warp = blockIdx.x * WARPS + threadIdx.x / 32, token = warp / a.parts, part = warp - token * a.parts;
     // rotation by halves pairs units u and u + rot / 16; what does not turn is dealt out in order
-    const int ru = a.interleaved ? 0 : a.rot_dim / 16;
-    const int ka = a.interleaved || ru == 0 ? l : l < ru ? l : 2 * l, kb = a.interleaved || ru == 0 ? l + LANES : l < ru ? l + ru : 2 * l + 1;
-    for (int task = blockIdx.y * WARPS + threadIdx.x / 32; task < tasks; task += WARPS * gridDim.y) {
-        const int role = task < wq ? 0 : task < wq + wk ? 1 : 2;
-        const int heads = role == 0 ? a.hq : a.hkv;
-        const int row = (task - (role == 0 ? 0 : role == 1 ? wq : wq + wk)) * RPW + sub;
-        bool live = row < n_tok * heads;
-        const int t = live ? row / heads : 0, h = live ? row - t * heads : 0;
-        if (DST != DST_ROWS) live = live && where[t].x >= 0;
-        const int ua = role == 2 ? l : ka, ub = role == 2 ? l + LANES : kb;
-        const __nv_bfloat16* src = role == 0 ? a.q + (tok0 + t) * a.q_stride : role == 1 ? a.k + (tok0 + t) * a.k_stride : a.v + (tok0 + t) * a.v_stride;
-        src += h * D;
-        uint4 ra = make_uint4(0, 0, 0, 0), rb = ra;
-        if (live) { ra = load_unit<VEC>(src + 8 * ua); rb = load_unit<VEC>(src + 8 * ub); }
-        float x[8], y[8];
-        unpack_unit(ra, x);
-        unpack_unit(rb, y);
-        if (role == 0) {
-            transform_row<D, float, float2>(a, a.q_weight, cs + t * half, ua, ub, x, y);
-            if (live) {
-                __nv_bfloat16* dst = a.q_out + (tok0 + t) * a.q_out_stride + h * D;
-                store_unit<VEC>(dst + 8 * ua, pack_unit(x));
-                store_unit<VEC>(dst + 8 * ub, pack_unit(y));
+    const int ru = IL ? 0 : a.rot_dim / 16;
+    const int ka = ru == 0 || l < ru ? l : 2 * l, kb = ru == 0 ? l + LANES : l < ru ? l + ru : 2 * l + 1;
+    novakv_grid_dependency_wait();
+    if (token >= a.n_tokens) return;
+
+    const int pos = a.tok_pos[token], seq = DST == DST_ROWS ? 0 : a.tok_seq[token];
+    const int step = a.parts * RPW, h0 = part * RPW;              // heads: a warp takes RPW at a time
+    struct Row { uint4 x, y; };
+    // (lanes behind the last head read it too: they take part, and write nothing)
+    auto fetch = [&](const __nv_bfloat16* rows, int h, int heads, int ua, int ub) {
+        const __nv_bfloat16* src = rows + min(h + sub, heads - 1) * D;
+        return Row{load_unit<VEC>(src + 8 * ua), load_unit<VEC>(src + 8 * ub)};
+    };
+    // q, then k, then v, counted through; a role's first rows are on their way while the angles, or the role before, are formed
+    const __nv_bfloat16 *q = a.q + token * a.q_stride, *k = a.k + token * a.k_stride, *v = a.v + token * a.v_stride;
+    const int nq = (a.hq + RPW - 1) / RPW * RPW, nk = (a.hkv + RPW - 1) / RPW * RPW;
+    auto first_k = [&](int h) { Row r = {}; if (h < nk) r = fetch(k, h, a.hkv, ka, kb); return r; };
+    auto first_v = [&](int h) { Row r = {}; if (DST != DST_ROWS && h < nk) r = fetch(v, h, a.hkv, l, l + LANES); return r; };
+    int h = h0;
+    Row next = h < nq ? fetch(q, h, a.hq, ka, kb) : h - nq < nk ? first_k(h - nq) : first_v(h - nq - nk);
+
+    int page = -1, slot = 0;                                      // -1: the token is skipped
+    if (DST != DST_ROWS && seq != -1) {
+        slot = pos % NOVAKV_PAGE_TOKENS;
+        if (seq < 0 || seq >= a.n_seq || pos < 0 || pos / NOVAKV_PAGE_TOKENS >= a.max_pages_per_seq) {
+            if (part == 0 && lane == 0) atomicOr(a.dev_status, NOVAKV_DEV_BAD_TOKEN);
+        } else {
+            page = a.page_table[(size_t)seq * a.max_pages_per_seq + pos / NOVAKV_PAGE_TOKENS];
+            if (page < 0 || page >= a.n_pages) {
+                if (part == 0 && lane == 0) atomicOr(a.dev_status, NOVAKV_DEV_BAD_PAGE);
+                page = -1;
+            } else if (part == 0 && lane == 0 && a.seq_lens[seq] <= pos) {     // (lengths only grow: a stale one costs an atomic)
+                atomicMax(&a.seq_lens[seq], pos + 1);
             }
-            continue;
         }
+    }
+    if (DST != DST_ROWS && page < 0) return;
+
+    // the lanes of a unit form its eight angles together: turns in binary64 (a far position keeps its angle), what is left of
+    // them in binary32
+    Turn turn;
+    {
+        constexpr int EACH = 8 / RPW;
+        float c[EACH], s[EACH];
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int i = sub * EACH + e;
+            c[e] = 1.f; s[e] = 0.f;
+            if (8 * (IL && i >= 4 ? kb : ka) < a.rot_dim) {
+                double turns = (double)pos * (double)a.inv_freq[angle_of<IL>(i, ka, kb)] * 0.15915494309189533577;
+                turns -= rint(turns);
+                sincospif(2.f * (float)turns, &s[e], &c[e]);
+                c[e] *= a.amplitude; s[e] *= a.amplitude;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            turn.c[i] = __shfl_sync(0xffffffffu, c[i % EACH], i / EACH * LANES + l);
+            turn.s[i] = __shfl_sync(0xffffffffu, s[i % EACH], i / EACH * LANES + l);
+        }
+    }
+    uint4 wx = make_uint4(0, 0, 0, 0), wy = wx;
+    bool norm = false;
+    auto weights_of = [&](const __nv_bfloat16* w) {
+        norm = w != nullptr;
+        if (norm) { wx = load_unit<false>(w + 8 * ka); wy = load_unit<false>(w + 8 * kb); }
+    };
+    if (h < nq) {
+        weights_of(a.q_weight);
+        __nv_bfloat16* out = a.q_out + token * a.q_out_stride + sub * D;
+#pragma unroll 1
+        for (; h < nq; h += step) {
+            const Row r = next;
+            next = h + step < nq ? fetch(q, h + step, a.hq, ka, kb) : first_k(h + step - nq);
+            float x[8], y[8];
+            unpack_unit(r.x, x);
+            unpack_unit(r.y, y);
+            transform_row<D, IL>(a, norm, wx, wy, turn, x, y);
+            if (h + sub < a.hq) {
+                store_unit<VEC>(out + h * D + 8 * ka, pack_unit(x));
+                store_unit<VEC>(out + h * D + 8 * kb, pack_unit(y));
+            }
+        }
+        if (h - nq >= nk) next = first_v(h - nq - nk);
+    }
+    h -= nq;
+    if (h < nk) {
+        weights_of(a.k_weight);
+#pragma unroll 1
+        for (; h < nk; h += step) {
+            const Row r = next;
+            next = h + step < nk ? fetch(k, h + step, a.hkv, ka, kb) : first_v(h + step - nk);
+            const bool live = h + sub < a.hkv;
+            float x[8], y[8];
+            unpack_unit(r.x, x);
+            unpack_unit(r.y, y);
+            bool sure = transform_row<D, IL>(a, norm, wx, wy, turn, x, y);
+            if constexpr (DST == DST_INT4) {
+                uint8_t* chunk = a.k_pages + ((size_t)page * a.hkv + h + sub) * I4Layout<D>::CHUNK_BYTES;
+                Quantised<D, true> code;
+                sure = code.template form<IL>(ka, kb, x, y) && sure;
+                if (__any_sync(0xffffffffu, live && !sure)) store_row64<D, IL>(a, pos, l, ka, kb, r.x, r.y, chunk, live);
+                else if (live) code.store(chunk, slot, l, ka, kb);
+            } else if (live) {
+                __nv_bfloat16* dst = DST == DST_ROWS ? a.k_out + token * a.k_out_stride + (h + sub) * D
+                                                     : reinterpret_cast<__nv_bfloat16*>(a.k_pages) + (((size_t)page * a.hkv + h + sub) * NOVAKV_PAGE_TOKENS + slot) * D;
+                store_unit<VEC>(dst + 8 * ka, pack_unit(x));
+                store_unit<VEC>(dst + 8 * kb, pack_unit(y));
+            }
+        }
+    }
+    if (DST == DST_ROWS) return;
+    h -= nk;
+#pragma unroll 1
+    for (; h < nk; h += step) {
+        const Row r = next;
+        next = first_v(h + step);
+        const bool live = h + sub < a.hkv;
         if constexpr (DST == DST_INT4) {
-            if (role == 1) {
-                double u[8], w[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) { u[i] = x[i]; w[i] = y[i]; }
-                transform_row<D, double, double2>(a, a.k_weight, cd + t * half, ua, ub, u, w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) { x[i] = (float)u[i]; y[i] = (float)w[i]; }
-            }
-            uint8_t* chunk = (role == 1 ? a.k_pages : a.v_pages) + ((size_t)max(where[t].x, 0) * a.hkv + h) * I4Layout<D>::CHUNK_BYTES;
-            store_row4<D>(chunk, where[t].y, l, ua, ub, x, y, live);
-            continue;
-        }
-        if (role == 1) transform_row<D, float, float2>(a, a.k_weight, cs + t * half, ua, ub, x, y);
-        if (live) {
-            __nv_bfloat16* dst;
-            if (DST == DST_ROWS) dst = a.k_out + (tok0 + t) * a.k_out_stride + h * D;
-            else
-                dst = reinterpret_cast<__nv_bfloat16*>(role == 1 ? a.k_pages : a.v_pages) +
-                      (((size_t)where[t].x * a.hkv + h) * NOVAKV_PAGE_TOKENS + where[t].y) * D;
-            store_unit<VEC>(dst + 8 * ua, role == 1 ? pack_unit(x) : ra);
-            store_unit<VEC>(dst + 8 * ub, role == 1 ? pack_unit(y) : rb);
+            float x[8], y[8];
+            unpack_unit(r.x, x);
+            unpack_unit(r.y, y);
+            Quantised<D, false> code;
+            code.template form<false>(l, l + LANES, x, y);
+            if (live) code.store(a.v_pages + ((size_t)page * a.hkv + h + sub) * I4Layout<D>::CHUNK_BYTES, slot, l, l, l + LANES);
+        } else if (live) {
+            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.v_pages) + (((size_t)page * a.hkv + h + sub) * NOVAKV_PAGE_TOKENS + slot) * D;
+            store_unit<VEC>(dst + 8 * l, r.x);
+            store_unit<VEC>(dst + 8 * (l + LANES), r.y);
         }
     }
 }
 
-// Read-back of the 4-bit cache: a row belongs to D / 16 lanes of 16 channels (8 code bytes) each.
+// Read-back of the 4-bit cache: a row belongs to D / 16 lanes, and what they store at a time lies side by side.
 struct GatherArgs {
     const int32_t *tok_seq, *tok_pos, *page_table;
     int n_tokens, hkv, n_pages, max_pages_per_seq, n_seq;
@@ -314,47 +465,55 @@ novakv_int4_gather_kernel(const GatherArgs a) {
         return;
     }
     const size_t tile = ((size_t)page * a.hkv + h) * Lay::CHUNK_BYTES + (pos % NOVAKV_PAGE_TOKENS / I4_TILE) * Lay::TILE_BYTES;
-    const int slot = pos % I4_TILE, at = Lay::word(slot, 2 * l), pair = Lay::pair(slot, l / 4);
-    uint2 code[2];
-    uint32_t meta[2];
+    // 16 bytes of a row at a time: 8 channels of bf16 or 4 of binary32
+    constexpr int CH = FP32 ? 4 : 8, N = D / (LANES * CH);
+    const int slot = pos % I4_TILE;
+    uint32_t code[2][N], meta[2][Lay::GROUPS];
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
         const uint8_t* src = (side ? a.v_pages : a.k_pages) + tile;
-        code[side] = *reinterpret_cast<const uint2*>(src + at);
-        meta[side] = *reinterpret_cast<const uint32_t*>(src + pair);
-    }
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const float scale = __uint_as_float(meta[side] << 16), zero = __uint_as_float(meta[side] & 0xffff0000u);
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            x[i] = fmaf(scale, (float)((i < 8 ? code[side].x >> (4 * i) : code[side].y >> (4 * i - 32)) & 15u), zero);
-        const size_t o = (size_t)row * D + 16 * l;
-        if (FP32) {
-            float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(side ? a.v_out : a.k_out) + o);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) dst[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-        } else {
-            uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(side ? a.v_out : a.k_out) + o);
-            dst[0] = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
-            dst[1] = make_uint4(pack2(x[8], x[9]), pack2(x[10], x[11]), pack2(x[12], x[13]), pack2(x[14], x[15]));
+        for (int i = 0; i < N; ++i) {
+            const int c = (i * LANES + l) * CH;
+            const uint8_t* at = src + Lay::word(slot, c / 8) + c % 8 / 2;
+            code[side][i] = FP32 ? *reinterpret_cast<const uint16_t*>(at) : *reinterpret_cast<const uint32_t*>(at);
         }
+#pragma unroll
+        for (int g = 0; g < Lay::GROUPS; ++g) meta[side][g] = *reinterpret_cast<const uint32_t*>(src + Lay::pair(slot, g));
     }
+#pragma unroll
+    for (int side = 0; side < 2; ++side)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = (i * LANES + l) * CH;
+            const uint32_t m = Lay::GROUPS == 1 || c < I4_GROUP ? meta[side][0] : meta[side][Lay::GROUPS - 1];
+            const float scale = __uint_as_float(m << 16), zero = __uint_as_float(m & 0xffff0000u);
+            float x[CH];
+#pragma unroll
+            for (int k = 0; k < CH; ++k) x[k] = fmaf(scale, (float)(code[side][i] >> (4 * k) & 15u), zero);
+            const size_t o = (size_t)row * D + c;
+            if constexpr (FP32)
+                *reinterpret_cast<float4*>(reinterpret_cast<float*>(side ? a.v_out : a.k_out) + o) = make_float4(x[0], x[1], x[2], x[3]);
+            else
+                *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(side ? a.v_out : a.k_out) + o) = pack_unit(x);
+        }
 }
 
-template <int D, int DST>
-novakv_status launch_rotate(novakv_ctx* ctx, RotateArgs& a, bool vec, cudaStream_t stream) {
-    const int half = a.rot_dim / 2;
-    a.tokens_per_block = a.n_tokens >= 8 * ctx->n_sm ? 4 : 1;
-    const size_t smem = (((size_t)a.tokens_per_block * half * 8 + 15) & ~(size_t)15) + (DST == DST_INT4 ? (size_t)a.tokens_per_block * half * 16 : 0) +
-                        a.tokens_per_block * sizeof(int2);
-    const dim3 grid((a.n_tokens + a.tokens_per_block - 1) / a.tokens_per_block);
-    const cudaError_t e = vec ? novakv_launch_pdl(novakv_rotate_kernel<D, DST, true>, grid, dim3(ROT_THREADS), smem, stream, a)
-                              : novakv_launch_pdl(novakv_rotate_kernel<D, DST, false>, grid, dim3(ROT_THREADS), smem, stream, a);
-    if (e != cudaSuccess) return NOVAKV_ECUDA;
+template <int D, int DST, bool IL>
+novakv_status launch_rotate_t(novakv_ctx* ctx, RotateArgs& a, bool vec, cudaStream_t stream) {
+    constexpr int RPW = 512 / D, WARPS = ROT_THREADS / 32;
+    const int nq = (a.hq + RPW - 1) / RPW, nk = (a.hkv + RPW - 1) / RPW, tasks = nq + (DST == DST_ROWS ? 1 : 2) * nk;
+    // a warp for each token, and several where there are fewer than some two waves of warps
+    a.parts = min(tasks, max(1, (64 * ctx->n_sm + a.n_tokens - 1) / a.n_tokens));
+    const long long blocks = ((long long)a.n_tokens * a.parts + WARPS - 1) / WARPS;
+    auto* kern = vec ? novakv_rotate_kernel<D, DST, true, IL> : novakv_rotate_kernel<D, DST, false, IL>;
+    if (novakv_launch_pdl(kern, dim3((unsigned)blocks), dim3(ROT_THREADS), 0, stream, a) != cudaSuccess) return NOVAKV_ECUDA;
     ctx->launches++;
     return NOVAKV_OK;
+}
+template <int D, int DST>
+novakv_status launch_rotate(novakv_ctx* ctx, RotateArgs& a, bool interleaved, bool vec, cudaStream_t stream) {
+    return interleaved ? launch_rotate_t<D, DST, true>(ctx, a, vec, stream) : launch_rotate_t<D, DST, false>(ctx, a, vec, stream);
 }
 
 // what all calls with a transform check of it
@@ -372,7 +531,6 @@ void set_transform(RotateArgs& a, const novakv_qk_transform* tr) {
     if (!tr) return;
     a.inv_freq = tr->inv_freq;
     a.rot_dim = tr->rot_dim;
-    a.interleaved = tr->interleaved;
     a.amplitude = tr->amplitude;
     a.q_weight = (const __nv_bfloat16*)tr->q_weight;
     a.k_weight = (const __nv_bfloat16*)tr->k_weight;
@@ -410,10 +568,11 @@ novakv_status append(novakv_ctx* ctx, const novakv_qk_transform* tr, const void*
     a.k_pages = (uint8_t*)k_pages; a.v_pages = (uint8_t*)v_pages;
     a.n_pages = n_pages; a.max_pages_per_seq = max_pages_per_seq; a.n_seq = n_seq;
     a.page_table = page_table; a.seq_lens = seq_lens; a.dev_status = ctx->dev_status;
+    const bool il = tr && tr->interleaved && tr->rot_dim > 0;
     const bool vec = rows_vec(k_new, k_stride) && rows_vec(v_new, v_stride) && (!q || (rows_vec(q, q_stride) && rows_vec(q_out, q_out_stride)));
     if (int4)
-        return d == 128 ? launch_rotate<128, DST_INT4>(ctx, a, vec, (cudaStream_t)stream) : launch_rotate<64, DST_INT4>(ctx, a, vec, (cudaStream_t)stream);
-    return d == 128 ? launch_rotate<128, DST_BF16>(ctx, a, vec, (cudaStream_t)stream) : launch_rotate<64, DST_BF16>(ctx, a, vec, (cudaStream_t)stream);
+        return d == 128 ? launch_rotate<128, DST_INT4>(ctx, a, il, vec, (cudaStream_t)stream) : launch_rotate<64, DST_INT4>(ctx, a, il, vec, (cudaStream_t)stream);
+    return d == 128 ? launch_rotate<128, DST_BF16>(ctx, a, il, vec, (cudaStream_t)stream) : launch_rotate<64, DST_BF16>(ctx, a, il, vec, (cudaStream_t)stream);
 }
 
 }  // namespace
@@ -439,8 +598,9 @@ extern "C" novakv_status novakv_qk_norm_rope(novakv_ctx* ctx, const novakv_qk_tr
     a.tok_pos = tok_pos;
     a.n_tokens = n_tokens; a.hq = q ? hq : 0; a.hkv = k ? hkv : 0;
     set_transform(a, tr);
+    const bool il = tr->interleaved && tr->rot_dim > 0;
     const bool vec = (!q || (rows_vec(q, q_stride) && rows_vec(q_out, q_out_stride))) && (!k || (rows_vec(k, k_stride) && rows_vec(k_out, k_out_stride)));
-    return d == 128 ? launch_rotate<128, DST_ROWS>(ctx, a, vec, (cudaStream_t)stream) : launch_rotate<64, DST_ROWS>(ctx, a, vec, (cudaStream_t)stream);
+    return d == 128 ? launch_rotate<128, DST_ROWS>(ctx, a, il, vec, (cudaStream_t)stream) : launch_rotate<64, DST_ROWS>(ctx, a, il, vec, (cudaStream_t)stream);
 }
 
 extern "C" novakv_status novakv_bf16_append(novakv_ctx* ctx, const novakv_qk_transform* tr, const void* k_new, long long k_stride,

@@ -42,7 +42,7 @@ def quantise(x):
     g = x.reshape(x.shape[:-1] + (x.shape[-1] // 64, 64))
     with np.errstate(all="ignore"):
         zero = to_bf16(g.min(-1, keepdims=True))
-        scale = to_bf16((g.max(-1, keepdims=True) - zero) / np.float32(15))
+        scale = to_bf16((g.max(-1, keepdims=True) - zero) * (np.float32(1) / np.float32(15)))
         scale = np.where((scale > 0) & np.isfinite(scale), scale, np.float32(1))
         t = np.rint((g - zero) / scale)
         codes = np.where(np.isnan(t), 0, np.clip(t, 0, 15)).astype(np.uint8)
