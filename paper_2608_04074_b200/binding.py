@@ -235,25 +235,19 @@ class Context:
         self._scale = float(head_dim) ** -0.5
         self._calls = _bind_calls(self.lib)
         self._operators = _bind_operators(self.lib, device, n_q_heads, n_kv_heads, head_dim)
+        self._fits = (head_dim, device)
 
     def _call(self, name, *args):
         status = self._calls[name](self.handle.value, *args)
         if status != 0:
             _check(self.lib, status, name)
 
-    def _operate(self, name, *args):
-        status = self._operators[name](self.handle.value, *args)
-        if status != 0:
-            _check(self.lib, status, name)
-
-    def _transform(self, transform):
-        """The transform, looked over once for each context that it is used with."""
-        if transform is not None and getattr(transform, "_checked", None) != (self.head_dim, self.cfg.device):
-            if not isinstance(transform, QKTransform):
-                raise TypeError("transform: a QKTransform or None")
-            transform.check(self.head_dim, self.cfg.device)
-            transform._checked = (self.head_dim, self.cfg.device)
-        return transform
+    def _look_over(self, transform):
+        """A transform's vectors have to fit the context: seen once for each context that it is used with."""
+        if not isinstance(transform, QKTransform):
+            raise TypeError("transform: a QKTransform or None")
+        transform.check(self.head_dim, self.cfg.device)
+        transform._checked = self._fits
 
     def close(self):
         if self.handle:
@@ -368,25 +362,39 @@ class Context:
     # -- between the projection and the cache; the 4-bit cache ---------------------------------
     def novakv_qk_norm_rope(self, transform, q, k, tok_pos, q_out, k_out):
         """Norms and rotation of q [n][Hq][d] and k [n][Hkv][d] (views with a token stride are taken; one side may be None)."""
-        self._operate("novakv_qk_norm_rope", self._transform(transform), q, k, tok_pos, q_out, k_out)
+        if transform is not None and getattr(transform, "_checked", None) is not self._fits:
+            self._look_over(transform)
+        status = self._operators["novakv_qk_norm_rope"](self.handle.value, transform, q, k, tok_pos, q_out, k_out)
+        if status:
+            _check(self.lib, status, "novakv_qk_norm_rope")
 
     def novakv_bf16_append(self, transform, k_new, v_new, tok_seq, tok_pos, k_pages_bf16, v_pages_bf16, page_table, seq_lens,
                            q=None, q_out=None):
         """Append to the BF16 paged cache, keys (and q, if given) through ``transform`` on the way (None: as they are)."""
-        self._operate("novakv_bf16_append", self._transform(transform), k_new, v_new, tok_seq, tok_pos, k_pages_bf16, v_pages_bf16,
-                      page_table, seq_lens, q, q_out)
+        if transform is not None and getattr(transform, "_checked", None) is not self._fits:
+            self._look_over(transform)
+        status = self._operators["novakv_bf16_append"](self.handle.value, transform, k_new, v_new, tok_seq, tok_pos, k_pages_bf16,
+                                                       v_pages_bf16, page_table, seq_lens, q, q_out)
+        if status:
+            _check(self.lib, status, "novakv_bf16_append")
 
     def novakv_int4_page_bytes(self):
         return int(self.lib.novakv_int4_page_bytes(self.handle))
 
     def novakv_int4_append(self, transform, k_new, v_new, tok_seq, tok_pos, k_pages, v_pages, page_table, seq_lens, q=None, q_out=None):
         """The same into the 4-bit paged cache."""
-        self._operate("novakv_int4_append", self._transform(transform), k_new, v_new, tok_seq, tok_pos, k_pages, v_pages, page_table,
-                      seq_lens, q, q_out)
+        if transform is not None and getattr(transform, "_checked", None) is not self._fits:
+            self._look_over(transform)
+        status = self._operators["novakv_int4_append"](self.handle.value, transform, k_new, v_new, tok_seq, tok_pos, k_pages, v_pages,
+                                                       page_table, seq_lens, q, q_out)
+        if status:
+            _check(self.lib, status, "novakv_int4_append")
 
     def novakv_int4_gather(self, tok_seq, tok_pos, k_pages, v_pages, page_table, k_out, v_out):
         """The values that slots of the 4-bit cache stand for, as rows [n][Hkv][d] in bf16 or float32."""
-        self._operate("novakv_int4_gather", tok_seq, tok_pos, k_pages, v_pages, page_table, k_out, v_out)
+        status = self._operators["novakv_int4_gather"](self.handle.value, tok_seq, tok_pos, k_pages, v_pages, page_table, k_out, v_out)
+        if status:
+            _check(self.lib, status, "novakv_int4_gather")
 
     def novakv_int4_workspace_bytes(self, batch):
         return int(self.lib.novakv_int4_workspace_bytes(self.handle, batch))
@@ -394,8 +402,10 @@ class Context:
     def novakv_int4_decode_attention(self, q, k_pages, v_pages, page_table, seq_lens, out, workspace, sm_scale=None, window=0,
                                      sink_logits=None):
         """Decode step over the 4-bit cache; ``window`` > 0: the last so many positions; ``sink_logits`` float32 [Hq] or None."""
-        self._operate("novakv_int4_decode_attention", q, k_pages, v_pages, page_table, seq_lens, out, workspace,
-                      self._scale if sm_scale is None else sm_scale, window, sink_logits)
+        status = self._operators["novakv_int4_decode_attention"](self.handle.value, q, k_pages, v_pages, page_table, seq_lens, out,
+                                                                 workspace, self._scale if sm_scale is None else sm_scale, window, sink_logits)
+        if status:
+            _check(self.lib, status, "novakv_int4_decode_attention")
 
     def novakv_last_device_status(self):
         word = c_uint32(0)

@@ -240,17 +240,23 @@ static long method_int(PyObject* x, PyObject* name) {
     Py_DECREF(n);
     return v;
 }
-/* sizes or strides of x into v; their number, or -1 */
-static int dims_of(PyObject* x, PyObject* name, int call, long long* v, int most) {
-    PyObject* s = call ? PyObject_CallMethodNoArgs(x, name) : PyObject_GetAttr(x, name);
-    if (!s) return -1;
+/* sizes or strides of x into v (the first `most`); their number, or -1 */
+static int dims_of(PyObject* s, long long* v, int most) {
     int n = -1;
-    if (PyTuple_Check(s)) {
+    if (s && PyTuple_Check(s)) {
         n = (int)PyTuple_GET_SIZE(s);
         for (int i = 0; i < n && i < most; ++i) v[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(s, i));
     }
-    Py_DECREF(s);
+    Py_XDECREF(s);
     return n;
+}
+/* What a call asks an argument for, once: an attribute of a tensor is a tenth of a microsecond. */
+typedef struct { long long size[4], stride[3]; int dims; } sizes;
+static int sizes_of(PyObject* x, sizes* z) {
+    if (z->dims >= 0) return 0;
+    z->dims = dims_of(PyObject_GetAttr(x, s_shape), z->size, 4);
+    if (z->dims < 0 && !PyErr_Occurred()) PyErr_SetString(PyExc_AttributeError, "shape");
+    return z->dims < 0 ? -1 : 0;
 }
 static int is_dtype(PyObject* x, PyObject* a, PyObject* b) {
     PyObject* t = PyObject_GetAttr(x, s_dtype);
@@ -258,44 +264,44 @@ static int is_dtype(PyObject* x, PyObject* a, PyObject* b) {
     return t && (t == a || t == b);
 }
 /* what is asked of argument `arg`; n: rows of the call, table_rows, pool_pages of its page table and its first pool */
-static int check(const Operator* e, char kind, int arg, PyObject* x, long long n, long long table_rows, long long pool_pages) {
+static int check(const Operator* e, char kind, int arg, PyObject* x, sizes* z, long long n, long long table_rows, long long pool_pages) {
     const int op = e->entry;
-    long long v[4] = {0, 0, 0, 0};
     if (method_int(x, s_get_device) != e->device) return refuse(op, arg, "has to be a tensor on the context's device");
+    if (kind != 'w' && sizes_of(x, z)) return -1;
+    const long long* v = z->size;
     switch (kind) {
         case 'q': case 'Q': case 'k': case 'K': {
             const long heads = kind == 'q' || kind == 'Q' ? e->hq : e->hkv;
             if (!is_dtype(x, bfloat16, bfloat16)) return refuse(op, arg, "has to be bfloat16");
-            if (dims_of(x, s_shape, 0, v, 4) != 3 || v[0] != n || v[1] != heads || v[2] != e->d) return refuse(op, arg, "has to be rows [n][heads][head_dim]");
-            if (dims_of(x, s_stride, 1, v, 4) != 3 || v[2] != 1 || (v[1] != e->d && heads > 1)) return refuse(op, arg, "has to have contiguous heads");
+            if (z->dims != 3 || v[0] != n || v[1] != heads || v[2] != e->d) return refuse(op, arg, "has to be rows [n][heads][head_dim]");
+            if (dims_of(PyObject_CallMethodNoArgs(x, s_stride), z->stride, 3) != 3 || z->stride[2] != 1 || (z->stride[1] != e->d && heads > 1))
+                return refuse(op, arg, "has to have contiguous heads");
             /* (decode attention takes no stride) */
-            if (kind == 'q' && n > 1 && v[0] != heads * e->d) return refuse(op, arg, "has to be contiguous");
+            if (kind == 'q' && n > 1 && z->stride[0] != heads * e->d) return refuse(op, arg, "has to be contiguous");
             return 0;
         }
         case 'e': case 'o':
             if (!is_dtype(x, bfloat16, float32)) return refuse(op, arg, "has to be bfloat16 or float32");
-            if (dims_of(x, s_shape, 0, v, 4) != 3 || v[0] != n || v[1] != (kind == 'o' ? e->hq : e->hkv) || v[2] != e->d) return refuse(op, arg, "has to be rows [n][heads][head_dim]");
+            if (z->dims != 3 || v[0] != n || v[1] != (kind == 'o' ? e->hq : e->hkv) || v[2] != e->d) return refuse(op, arg, "has to be rows [n][heads][head_dim]");
             break;
         case 'i':
-            if (!is_dtype(x, int32, int32) || dims_of(x, s_shape, 0, v, 4) != 1 || v[0] != n) return refuse(op, arg, "has to be int32, one for each row");
+            if (!is_dtype(x, int32, int32) || z->dims != 1 || v[0] != n) return refuse(op, arg, "has to be int32, one for each row");
             break;
         case 't':
-            if (!is_dtype(x, int32, int32) || dims_of(x, s_shape, 0, v, 4) != 2) return refuse(op, arg, "has to be an int32 table [sequences][pages]");
+            if (!is_dtype(x, int32, int32) || z->dims != 2) return refuse(op, arg, "has to be an int32 table [sequences][pages]");
             break;
         case 'l':
-            if (!is_dtype(x, int32, int32) || dims_of(x, s_shape, 0, v, 4) != 1 || v[0] != table_rows) return refuse(op, arg, "has to be int32, one for each row of the page table");
+            if (!is_dtype(x, int32, int32) || z->dims != 1 || v[0] != table_rows) return refuse(op, arg, "has to be int32, one for each row of the page table");
             break;
         case 'f':
-            if (!is_dtype(x, float32, float32) || dims_of(x, s_shape, 0, v, 4) != 1 || v[0] != e->hq) return refuse(op, arg, "has to be float32, one for each query head");
+            if (!is_dtype(x, float32, float32) || z->dims != 1 || v[0] != e->hq) return refuse(op, arg, "has to be float32, one for each query head");
             break;
-        case 'b': case 'c': {
-            long long bytes;
-            PyObject* b = PyObject_GetAttr(x, s_nbytes);
-            if (!b) return -1;
-            bytes = PyLong_AsLongLong(b);
-            Py_DECREF(b);
+        case 'b': case 'c': {                              /* [pages] and any dimensions behind, of a page's bytes in all */
+            long long page = kind == 'b' ? 2 : 1;
+            for (int i = 1; i < z->dims && i < 4; ++i) page *= v[i];
             const long long row = kind == 'b' ? e->d * 2 : e->d / 2 + e->d / 64 * 4;
-            if (!is_dtype(x, kind == 'b' ? bfloat16 : uint8, NULL) || bytes != pool_pages * e->hkv * 64 * row || shape_of(x, 0) != pool_pages) return refuse(op, arg, "has to be a pool of this cache's pages, as many as the keys' pool");
+            if (!is_dtype(x, kind == 'b' ? bfloat16 : uint8, NULL) || z->dims < 2 || z->dims > 4 || v[0] != pool_pages || page != e->hkv * 64 * row)
+                return refuse(op, arg, "has to be a pool of this cache's pages, as many as the keys' pool");
             break;
         }
         default: break;
@@ -333,12 +339,17 @@ static PyObject* operator_call(PyObject* self, PyObject* const* args, size_t nar
     }
     const unsigned long long ctx = args[0] == Py_None ? 0 : PyLong_AsUnsignedLongLong(args[0]);
     if (PyErr_Occurred()) return NULL;
-    const long long n = shape_of(args[1 + operators[op].rows], 0);
-    if (PyErr_Occurred()) return NULL;
-    const long long table_rows = operators[op].table < 0 ? 0 : shape_of(args[1 + operators[op].table], 0);
-    if (PyErr_Occurred()) return NULL;
-    const long long pool_pages = operators[op].pool < 0 ? 0 : shape_of(args[1 + operators[op].pool], 0);
-    if (PyErr_Occurred()) return NULL;
+    sizes z[MAX_ARGS];
+    for (int i = 0; i < operators[op].n_args; ++i) z[i].dims = -1;
+    const int asked[3] = {operators[op].rows, operators[op].table, operators[op].pool};
+    long long first[3] = {0, 0, 0};                        /* shape[0] of each */
+    for (int i = 0; i < 3; ++i) {
+        if (asked[i] < 0) continue;
+        if (sizes_of(args[1 + asked[i]], &z[asked[i]])) return NULL;
+        if (z[asked[i]].dims < 1) { refuse(op, asked[i], "has no dimension"); return NULL; }
+        first[i] = z[asked[i]].size[0];
+    }
+    const long long n = first[0], table_rows = first[1], pool_pages = first[2];
     if (op == INT4_DECODE && n != table_rows) { refuse(op, operators[op].table, "has to have one row for each query"); return NULL; }
     if (n > 0x7fffffff || pool_pages > 0x7fffffff) { refuse(op, 0, "is too large"); return NULL; }
     long long a[MAX_ARGS];
@@ -348,14 +359,13 @@ static PyObject* operator_call(PyObject* self, PyObject* const* args, size_t nar
         const int arg = p[i].arg;
         PyObject* x = args[1 + arg];
         unsigned long long u = 0;
-        long long v[4] = {0, 0, 0, 0};
         a[i] = 0;
         switch (p[i].kind) {
             case 'Q': case 'K': case 'f':
                 if (x == Py_None) break;                   /* fall through */
             case 'q': case 'k': case 'e': case 'o': case 'i': case 't': case 'l': case 'b': case 'c': case 'w':
                 if (x == Py_None) { refuse(op, arg, "is missing"); return NULL; }
-                if (check(e, p[i].kind, arg, x, n, table_rows, pool_pages) || pointer_of(x, &u)) return NULL;
+                if (check(e, p[i].kind, arg, x, &z[arg], n, table_rows, pool_pages) || pointer_of(x, &u)) return NULL;
                 a[i] = (long long)u;
                 break;
             case 'h': case 'H':
@@ -364,13 +374,12 @@ static PyObject* operator_call(PyObject* self, PyObject* const* args, size_t nar
                 a[i] = (long long)u;
                 break;
             case 's':
-                if (x == Py_None) break;
-                if (dims_of(x, s_stride, 1, v, 4) != 3) { refuse(op, arg, "has to be rows"); return NULL; }
-                a[i] = n > 1 ? v[0] : e->hq * e->d;        /* (of a single row any stride is one) */
+                if (x == Py_None) break;                   /* (behind its rows: they have been looked at) */
+                a[i] = n > 1 ? z[arg].stride[0] : e->hq * e->d;        /* (of a single row any stride is one) */
                 break;
             case 'N': a[i] = n; break;
-            case '0': a[i] = shape_of(x, 0); break;
-            case '1': a[i] = shape_of(x, 1); break;
+            case '0': a[i] = z[arg].size[0]; break;
+            case '1': a[i] = z[arg].size[1]; break;
             case 'I': if (as_int(x, 0, &a[i])) return NULL; break;
             case 'F': f = (float)PyFloat_AsDouble(x); break;
             case 'T': a[i] = is_dtype(x, float32, float32); break;

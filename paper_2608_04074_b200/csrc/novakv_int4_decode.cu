@@ -344,7 +344,7 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
         // ---- a (sequence, KV head) pair: its queries as the products' columns
         const int seg_first = at.unit, seg_n = min(at.s.units - at.unit, n - t);
         uint32_t qf[NP][2][2];
-        float qfac, qz0[G], qz1[G];
+        float qfac, qz0[G], qz1[G], mid0[G], mid1[G];                // (mid: FINE alone, -8 times the sums of q as the products have it)
         {
             const __nv_bfloat16* qp = a.q + (((size_t)at.b * a.hkv + at.kvh) * HG + gr % COLS % HG) * D + 8 * j;
             uint4 w[NP];
@@ -384,6 +384,11 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
             for (int g = 0; g < G; ++g) {
                 sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 1);
                 sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 2);
+                if (FINE) {                                       // codes are counted from the middle, 8: what is taken off is small
+                    const float u = sum[g] * f * -0x1p-15f;
+                    mid0[g] = __shfl_sync(0xffffffffu, u, 8 * jj);
+                    mid1[g] = __shfl_sync(0xffffffffu, u, 8 * jj + 4);
+                }
                 qz0[g] = a.scale_log2 * __shfl_sync(0xffffffffu, sum[g], 8 * jj);     // (lane 4 c holds column c)
                 qz1[g] = a.scale_log2 * __shfl_sync(0xffffffffu, sum[g], 8 * jj + 4);
             }
@@ -414,7 +419,7 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
 #pragma unroll
                 for (int g = 0; g < G; ++g)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[g][i] = 0.f;
+                    for (int i = 0; i < 4; ++i) acc[g][i] = !FINE ? 0.f : (i & 1) ? mid1[g] : mid0[g];
 #pragma unroll
                 for (int pp = 0; pp < NP; pp += 2) {
                     uint32_t r[4];
@@ -437,7 +442,8 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
                     float d0 = 0.f, d1 = 0.f;
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        const float scale = __uint_as_float(w[g] << 16) * qfac, zero = __uint_as_float(w[g] & 0xffff0000u);
+                        const float step = __uint_as_float(w[g] << 16), scale = step * qfac;
+                        const float zero = FINE ? fmaf(8.f, step, __uint_as_float(w[g] & 0xffff0000u)) : __uint_as_float(w[g] & 0xffff0000u);
                         const float c0 = SPLIT ? (up ? acc[g][2] : acc[g][0]) : acc[g][2 * r], c1 = SPLIT ? (up ? acc[g][3] : acc[g][1]) : acc[g][2 * r + 1];
                         d0 = fmaf(scale, c0, g ? fmaf(zero, qz0[g], d0) : zero * qz0[g]);
                         d1 = fmaf(scale, c1, g ? fmaf(zero, qz1[g], d1) : zero * qz1[g]);
@@ -512,45 +518,81 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
                 }
             }
 
-            // ---- weights and values
+            // ---- weights and values.  FINE: sums of 32 tokens apart, on codes counted from the middle (a product with the constant
+            // -8 of all of them), added in binary32: the tensor core cuts sums off instead of rounding them, which over a long
+            // sequence of like weights would add up against a result that is small beside them.
+            constexpr int SB = FINE ? 2 : 1;
 #pragma unroll
-            for (int s = 0; s < S; ++s) {
-                uint32_t b_hi[G][2], b_lo[G][2];
+            for (int sb = 0; sb < S; sb += SB) {
+                uint32_t b_hi[SB][G][2], b_lo[SB][G][2];
+                float mid[G][4];
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const float p0 = ex2f(z0[s][r] - m0), p1 = ex2f(z1[s][r] - m1);
-                    l0 += p0; l1 += p1;
+                for (int e = 0; e < SB; ++e) {
+                    const int s = sb + e;
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const float p0 = ex2f(z0[s][r] - m0), p1 = ex2f(z1[s][r] - m1);
+                        l0 += p0; l1 += p1;
+#pragma unroll
+                        for (int g = 0; g < G; ++g) {
+                            const float zero = FINE ? fmaf(8.f, vs[s][r][g], vz[s][r][g]) : vz[s][r][g];
+                            zs0[g] = fmaf(p0, zero, zs0[g]);
+                            zs1[g] = fmaf(p1, zero, zs1[g]);
+                            const float f = vfac * vs[s][r][g], w0 = p0 * f, w1 = p1 * f;
+                            const uint32_t hi16 = pack_half(w0, w1), x = movmatrix_t(hi16);
+                            // SPLIT: columns 0..3 take the lower eight tokens, columns 4..7 the upper ones
+                            if (SPLIT) { b_hi[e][g][0] = gr < 4 ? x : 0u; b_hi[e][g][1] = gr < 4 ? 0u : x; }
+                            else b_hi[e][g][r] = x;
+                            if (FINE) {
+                                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi16));
+                                const uint32_t y = movmatrix_t(pack_half(w0 - back.x, w1 - back.y));
+                                if (SPLIT) { b_lo[e][g][0] = gr < 4 ? y : 0u; b_lo[e][g][1] = gr < 4 ? 0u : y; }
+                                else b_lo[e][g][r] = y;
+                            }
+                        }
+                    }
+                }
+                if (FINE) {
+                    constexpr uint32_t M8 = 0x82008200u;          // -8 2^-18 twice
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        zs0[g] = fmaf(p0, vz[s][r][g], zs0[g]);
-                        zs1[g] = fmaf(p1, vz[s][r][g], zs1[g]);
-                        const float f = vfac * vs[s][r][g], w0 = p0 * f, w1 = p1 * f;
-                        const uint32_t hi16 = pack_half(w0, w1), x = movmatrix_t(hi16);
-                        // SPLIT: columns 0..3 take the lower eight tokens, columns 4..7 the upper ones
-                        if (SPLIT) { b_hi[g][0] = gr < 4 ? x : 0u; b_hi[g][1] = gr < 4 ? 0u : x; }
-                        else b_hi[g][r] = x;
-                        if (FINE) {
-                            const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi16));
-                            const uint32_t y = movmatrix_t(pack_half(w0 - back.x, w1 - back.y));
-                            if (SPLIT) { b_lo[g][0] = gr < 4 ? y : 0u; b_lo[g][1] = gr < 4 ? 0u : y; }
-                            else b_lo[g][r] = y;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mid[g][i] = 0.f;
+#pragma unroll
+                        for (int e = 0; e < SB; ++e) {
+                            mma16816(mid[g], M8, M8, M8, M8, b_hi[e][g][0], b_hi[e][g][1]);
+                            mma16816(mid[g], M8, M8, M8, M8, b_lo[e][g][0], b_lo[e][g][1]);
                         }
                     }
                 }
 #pragma unroll
                 for (int pp = 0; pp < NP; pp += 2) {
-                    uint32_t r[4];
-                    ldmatrix4t((vbase + mat ^ pp << 4) + s / 2 * TB + s % 2 * 16 * Lay::ROW, r);
+                    uint32_t r[SB][4];
+#pragma unroll
+                    for (int e = 0; e < SB; ++e) ldmatrix4t((vbase + mat ^ pp << 4) + (sb + e) / 2 * TB + (sb + e) % 2 * 16 * Lay::ROW, r[e]);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        uint32_t x[4], y[4];
                         const int p = pp + h, g = p / 2;
-                        unpack_codes<FINE>(r[2 * h], x);
-                        unpack_codes<FINE>(r[2 * h + 1], y);
+                        uint32_t x[SB][4], y[SB][4];
+#pragma unroll
+                        for (int e = 0; e < SB; ++e) {
+                            unpack_codes<FINE>(r[e][2 * h], x[e]);
+                            unpack_codes<FINE>(r[e][2 * h + 1], y[e]);
+                        }
 #pragma unroll
                         for (int sh = 0; sh < 2; ++sh) {
-                            mma16816(o[p][sh], x[2 * sh], x[2 * sh + 1], y[2 * sh], y[2 * sh + 1], b_hi[g][0], b_hi[g][1]);
-                            if (FINE) mma16816(o[p][sh], x[2 * sh], x[2 * sh + 1], y[2 * sh], y[2 * sh + 1], b_lo[g][0], b_lo[g][1]);
+                            if (!FINE) {
+                                mma16816(o[p][sh], x[0][2 * sh], x[0][2 * sh + 1], y[0][2 * sh], y[0][2 * sh + 1], b_hi[0][g][0], b_hi[0][g][1]);
+                            } else {
+                                float sum[4] = {mid[g][0], mid[g][1], mid[g][2], mid[g][3]};
+#pragma unroll
+                                for (int e = 0; e < SB; ++e) {
+                                    mma16816(sum, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_hi[e][g][0], b_hi[e][g][1]);
+                                    mma16816(sum, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_lo[e][g][0], b_lo[e][g][1]);
+                                }
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) o[p][sh][i] += sum[i];
+                            }
                         }
                     }
                 }

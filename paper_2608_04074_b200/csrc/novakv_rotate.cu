@@ -77,11 +77,16 @@ __device__ __forceinline__ uint4 pack_unit(const T (&x)[8]) {
 // minimum and maximum that keep a NaN: a group that holds one gets it as its zero
 __device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float min_nan(float a, float b, float c) { float r; asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+__device__ __forceinline__ float max_nan(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 
 // What a lane knows of its token and layer: (cos, sin) of its eight pairs - (x_i, y_i), or neighbours (IL) x_2i, x_2i+1 for i < 4
-// and y_2i-8, y_2i-7 - and its channels' weights.
+// and y_2i-8, y_2i-7 - and its channels' weights as they are given.  (The weights taken into the cosines would save an eighth of
+// the instructions, and cost the registers of two more blocks an SM: a prompt of 16384 tokens, d = 64, 51.5 against 56 us.)
 struct Turn {
     float c[8], s[8];
+    uint4 wx, wy;
+    bool norm;
 };
 // the angle of a lane's pair i
 template <bool IL>
@@ -91,13 +96,13 @@ __device__ __forceinline__ float& first_of(int i, float (&x)[8], float (&y)[8]) 
 template <bool IL>
 __device__ __forceinline__ float& second_of(int i, float (&x)[8], float (&y)[8]) { return !IL ? y[i] : i < 4 ? x[2 * i + 1] : y[2 * i - 7]; }
 
-// norm (wx, wy: the units' weights) and rotation of a row's two units.  All lanes of the warp take part.  False where the sum of
-// squares leaves the range in which its roundings are relative ones.
+// norm and rotation of a row's two units.  All lanes of the warp take part.  False where the sum of squares leaves the range in
+// which its roundings are relative ones.
 template <int D, bool IL>
-__device__ __forceinline__ bool transform_row(const RotateArgs& a, bool norm, const uint4& wx, const uint4& wy, const Turn& turn, float (&x)[8], float (&y)[8]) {
+__device__ __forceinline__ bool transform_row(const RotateArgs& a, const Turn& turn, int ua, int ub, float (&x)[8], float (&y)[8]) {
     constexpr int LANES = D / 16;
     bool fine = true;
-    if (norm) {
+    if (turn.norm) {
         float ss = 0.f, st = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) { ss = fmaf(x[i], x[i], ss); st = fmaf(y[i], y[i], st); }
@@ -107,15 +112,16 @@ __device__ __forceinline__ bool transform_row(const RotateArgs& a, bool norm, co
         const float r = rsqrtf(fmaf(ss, 1.f / D, a.eps));
         fine = ss > 1e-30f && ss < 1e30f;
         float w[8];
-        unpack_unit(wx, w);
+        unpack_unit(turn.wx, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] *= r * w[i];
-        unpack_unit(wy, w);
+        unpack_unit(turn.wy, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] *= r * w[i];
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {                                 // (a pair that is not rotated has the angle 0)
+    for (int i = 0; i < 8; ++i) {                                 // (what is not rotated is left alone: infinity times 0 would be NaN)
+        if (8 * (IL && i >= 4 ? ub : ua) >= a.rot_dim) continue;
         float &p = first_of<IL>(i, x, y), &q = second_of<IL>(i, x, y);
         const float u = p * turn.c[i] - q * turn.s[i];
         q = q * turn.c[i] + p * turn.s[i];
@@ -138,8 +144,8 @@ constexpr float ROUND = 12582912.f;          // 1.5 2^23: added and taken away a
 
 // Codes and pairs of a row.  All lanes of the warp take part.
 // A value row is given exactly.  A key (KEY) is defined by binary64, but formed in binary32 first: each element is off by less
-// than 2^-19 (|a| + |b|) of the pair it comes from (a mean of D squares, a root, the weight, cos and sin, two products and a sum:
-// 29 roundings of 2^-24), which is at most sqrt(2) times that of the pair it gives.  Where no element, minimum or maximum can
+// than 2^-19 (|a| + |b|) of the pair it comes from (a mean of D squares and its root 14 roundings of 2^-24, cos and sin 5, far
+// positions 4, their products with weight, element and root 3, a sum 1: less than 32), which is at most sqrt(2) times that of the pair it gives.  Where no element, minimum or maximum can
 // have crossed a border of its rounding by that, codes and pairs are those of the binary64 key; else the answer is false, and
 // the row is formed again in binary64: some 3 % of the warps' rows.
 template <int D, bool KEY>
@@ -147,36 +153,32 @@ struct Quantised {
     uint32_t wx, wy;
     float zero[I4Layout<D>::GROUPS], scale[I4Layout<D>::GROUPS];
 
-    template <bool INTERLEAVED>
+    // APART: the units lie in a group each (d = 64: in the one there is)
+    template <bool INTERLEAVED, bool APART>
     __device__ __forceinline__ bool form(int ua, int ub, const float (&x)[8], const float (&y)[8]) {
         constexpr int G = I4Layout<D>::GROUPS, LANES = D / 16;
         constexpr float OFF = 2.75e-6f;                           // sqrt(2) 2^-19 = 2.70e-6
         bool sure = true, ranged = true;
         float dx[8], dy[8];
-        float xl = x[0], xh = x[0], yl = y[0], yh = y[0], xl2, xh2, yl2, yh2;
-        if (KEY) {
+        float xl, xh, yl, yh, xl2 = 0.f, xh2 = 0.f, yl2 = 0.f, yh2 = 0.f;
+        if (!KEY) {
+            extremes(x, xl, xh);
+            extremes(y, yl, yh);
+        } else {
+            float ux[8], uy[8], lx[8], ly[8];                     // upper and lower ends
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 dx[i] = OFF * (fabsf(x[i]) + fabsf(INTERLEAVED ? x[i ^ 1] : y[i]));
                 dy[i] = INTERLEAVED ? OFF * (fabsf(y[i]) + fabsf(y[i ^ 1])) : dx[i];
+                ux[i] = x[i] + dx[i]; uy[i] = y[i] + dy[i];
+                lx[i] = x[i] - dx[i]; ly[i] = y[i] - dy[i];
             }
-            // upper ends in xl, xh, yl, yh, lower ends in the others; of the lower ends fmin passes a NaN over, the upper keep it
-            xl = xh = x[0] + dx[0]; yl = yh = y[0] + dy[0];
-            xl2 = xh2 = x[0] - dx[0]; yl2 = yh2 = y[0] - dy[0];
-        }
-#pragma unroll
-        for (int i = 1; i < 8; ++i) {
-            const float u = KEY ? x[i] + dx[i] : x[i], v = KEY ? y[i] + dy[i] : y[i];
-            xl = min_nan(xl, u); xh = max_nan(xh, u);
-            yl = min_nan(yl, v); yh = max_nan(yh, v);
-            if (KEY) {
-                xl2 = fminf(xl2, x[i] - dx[i]); yl2 = fminf(yl2, y[i] - dy[i]);
-                xh2 = fmaxf(xh2, x[i] - dx[i]); yh2 = fmaxf(yh2, y[i] - dy[i]);
-            }
+            extremes(ux, xl, xh); extremes(uy, yl, yh);
+            extremes(lx, xl2, xh2); extremes(ly, yl2, yh2);
         }
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            const bool xin = G == 1 || ua / 8 == g, yin = G == 1 || ub / 8 == g;
+            const bool xin = G == 1 || (APART ? g == 0 : ua / 8 == g), yin = G == 1 || (APART ? g == 1 : ub / 8 == g);
             float lo = min_nan(xin ? xl : CUDART_INF_F, yin ? yl : CUDART_INF_F), hi = max_nan(xin ? xh : -CUDART_INF_F, yin ? yh : -CUDART_INF_F);
             if (!KEY) {
 #pragma unroll
@@ -188,45 +190,70 @@ struct Quantised {
                 scale[g] = scale_of(hi, zero[g]);
                 ranged = ranged && zero[g] > -1e28f && hi < 1e28f && scale[g] > 1e-28f;
             } else {
-                const float lo2 = fminf(xin ? xl2 : CUDART_INF_F, yin ? yl2 : CUDART_INF_F);
-                float hi2 = fmaxf(xin ? xh2 : -CUDART_INF_F, yin ? yh2 : -CUDART_INF_F);
+                const float lo2 = min_nan(xin ? xl2 : CUDART_INF_F, yin ? yl2 : CUDART_INF_F);
+                float hi2 = max_nan(xin ? xh2 : -CUDART_INF_F, yin ? yh2 : -CUDART_INF_F);
                 __nv_bfloat162 both = __floats2bfloat162_rn(lo, lo2);   // (rounding keeps the order)
 #pragma unroll
                 for (int s = 1; s < LANES; s <<= 1) {
                     const uint32_t o = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t*>(&both), s);
                     both = __hmin2_nan(both, *reinterpret_cast<const __nv_bfloat162*>(&o));
                     hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, s));
-                    hi2 = fmaxf(hi2, __shfl_xor_sync(0xffffffffu, hi2, s));
+                    hi2 = max_nan(hi2, __shfl_xor_sync(0xffffffffu, hi2, s));
                 }
                 zero[g] = __low2float(both);
                 scale[g] = scale_of(hi, zero[g]);
                 sure = sure && zero[g] == __high2float(both) && scale[g] == scale_of(hi2, zero[g]) && scale[g] > 1e-28f && zero[g] > -1e28f && hi < 1e28f;
             }
         }
-        const int ga = G == 1 ? 0 : ua / 8, gb = G == 1 ? 0 : ub / 8;
+        const int ga = G == 1 || APART ? 0 : ua / 8, gb = G == 1 ? 0 : APART ? 1 : ub / 8;
         const float zx = ga ? zero[G - 1] : zero[0], zy = gb ? zero[G - 1] : zero[0];
         const Divisor qx(ga ? scale[G - 1] : scale[0]), qy(gb ? scale[G - 1] : scale[0]);
-        float worst = 0.f;                                        // of the distances from the codes, errors included
-        wx = unit(x, dx, zx, qx, worst);
-        wy = unit(y, dy, zy, qy, worst);
-        if (!KEY && !ranged) {
+        if (KEY) {
+            float worst = 0.f;
+            wx = unit_near(x, dx, zx, qx.r, worst);
+            wy = unit_near(y, dy, zy, qy.r, worst);
+            return sure && worst < 0.5f;
+        }
+        wx = unit(x, zx, qx);
+        wy = unit(y, zy, qy);
+        if (!ranged) {
             wx = unit_divided(x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7], zx, qx.s);
             wy = unit_divided(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7], zy, qy.s);
         }
-        // (difference and quotient themselves are off by 2e-6 at most, here and where they are defined)
-        return sure && worst < 0.499992f;
+        return true;
     }
-    // the code word of a unit: two times four codes as a number of 16 bits
-    static __device__ __forceinline__ uint32_t unit(const float (&x)[8], const float (&d)[8], float zero, const Divisor& by, float& worst) {
+    // four codes as a number of 16 bits, twice
+    static __device__ __forceinline__ uint32_t pack_codes(const float (&c)[8]) {
         float half[2];
 #pragma unroll
-        for (int i = 7; i >= 0; --i) {
-            const float t = fminf(fmaxf(by.quotient(x[i] - zero), 0.f), 15.f);        // (a NaN gets code 0)
-            const float c = __fadd_rn(__fadd_rn(t, ROUND), -ROUND);
-            if (KEY) worst = fmaxf(worst, fmaf(d[i], by.r, fabsf(t - c)));
-            half[i / 4] = i % 4 == 3 ? c : fmaf(half[i / 4], 16.f, c);
-        }
+        for (int i = 7; i >= 0; --i) half[i / 4] = i % 4 == 3 ? c[i] : fmaf(half[i / 4], 16.f, c[i]);
         return __byte_perm(__float_as_uint(half[0] + 8388608.f), __float_as_uint(half[1] + 8388608.f), 0x5410);
+    }
+    static __device__ __forceinline__ void extremes(const float (&x)[8], float& lo, float& hi) {
+        lo = min_nan(min_nan(x[0], x[1], x[2]), min_nan(x[3], x[4], x[5]), min_nan(x[6], x[7]));
+        hi = max_nan(max_nan(x[0], x[1], x[2]), max_nan(x[3], x[4], x[5]), max_nan(x[6], x[7]));
+    }
+    // the code word of a unit
+    static __device__ __forceinline__ uint32_t unit(const float (&x)[8], float zero, const Divisor& by) {
+        float c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)                               // (a NaN gets code 0)
+            c[i] = __fadd_rn(__fadd_rn(fminf(fmaxf(by.quotient(x[i] - zero), 0.f), 15.f), ROUND), -ROUND);
+        return pack_codes(c);
+    }
+    // The same of a key, not to the last bit: t = (x - zero) r / 15 in [0, 1] by one multiply-add that saturates, and how far
+    // 15 t can be from its code at most: the element's own error, roundings of 1 / s, 1 / 15, their product and the zero's, at most
+    // 2^-24 (7 |zero| / s + 63), and what difference and quotient are off by where the code is defined, 2^-24 31.
+    static __device__ __forceinline__ uint32_t unit_near(const float (&x)[8], const float (&d)[8], float zero, float r, float& worst) {
+        const float r15 = r * (1.f / 15.f), z15 = -zero * r15, off = fmaf(fabsf(z15), 7e-6f, 7e-6f);
+        float c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float t = __saturatef(fmaf(x[i], r15, z15));
+            c[i] = __fadd_rn(__fmaf_rn(t, 15.f, ROUND), -ROUND);
+            worst = fmaxf(worst, fmaf(d[i], r, fabsf(fmaf(t, 15.f, -c[i]))) + off);
+        }
+        return pack_codes(c);
     }
     static __device__ __noinline__ uint32_t unit_divided(float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7, float zero, float scale) {
         const float x[8] = {x0, x1, x2, x3, x4, x5, x6, x7};
@@ -275,22 +302,33 @@ __device__ __noinline__ void store_row64(const RotateArgs& a, int pos, int l, in
             y[i] *= r * (double)__bfloat162float(a.k_weight[8 * ub + i]);
         }
     }
-    const double amp = a.amplitude;
+    // (the lanes of a unit form its angles together here, too)
+    constexpr int RPW = 32 / LANES, EACH = 8 / RPW;
+    const int sub = (threadIdx.x & 31) / LANES;
+    double c[EACH], s[EACH];
 #pragma unroll 1
+    for (int e = 0; e < EACH; ++e) {
+        const int i = sub * EACH + e;
+        double se = 0.0, ce = 1.0;
+        if (8 * (IL && i >= 4 ? ub : ua) < a.rot_dim) {
+            sincos((double)pos * (double)a.inv_freq[angle_of<IL>(i, ua, ub)], &se, &ce);
+            ce *= (double)a.amplitude; se *= (double)a.amplitude;
+        }
+        if (e == 0) { c[0] = ce; s[0] = se; } else { c[EACH - 1] = ce; s[EACH - 1] = se; }
+    }
+#pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int f = angle_of<IL>(i, ua, ub);
+        const double ci = __shfl_sync(0xffffffffu, c[i % EACH], i / EACH * LANES + l), si = __shfl_sync(0xffffffffu, s[i % EACH], i / EACH * LANES + l);
         if (8 * (IL && i >= 4 ? ub : ua) >= a.rot_dim) continue;
-        double s, c;
-        sincos((double)pos * (double)a.inv_freq[f], &s, &c);
         double &p = !IL ? x[i] : i < 4 ? x[2 * i] : y[2 * i - 8], &q = !IL ? y[i] : i < 4 ? x[2 * i + 1] : y[2 * i - 7];
-        const double v = amp * (p * c - q * s);
-        q = amp * (q * c + p * s);
+        const double v = p * ci - q * si;
+        q = q * ci + p * si;
         p = v;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) { xo[i] = (float)x[i]; yo[i] = (float)y[i]; }
     Quantised<D, false> code;
-    code.template form<false>(ua, ub, xo, yo);
+    code.template form<false, false>(ua, ub, xo, yo);
     if (live) code.store(chunk, pos % NOVAKV_PAGE_TOKENS, l, ua, ub);
 }
 
@@ -362,11 +400,9 @@ novakv_rotate_kernel(const __grid_constant__ RotateArgs a) {
             turn.s[i] = __shfl_sync(0xffffffffu, s[i % EACH], i / EACH * LANES + l);
         }
     }
-    uint4 wx = make_uint4(0, 0, 0, 0), wy = wx;
-    bool norm = false;
     auto weights_of = [&](const __nv_bfloat16* w) {
-        norm = w != nullptr;
-        if (norm) { wx = load_unit<false>(w + 8 * ka); wy = load_unit<false>(w + 8 * kb); }
+        turn.norm = w != nullptr;
+        if (turn.norm) { turn.wx = load_unit<false>(w + 8 * ka); turn.wy = load_unit<false>(w + 8 * kb); }
     };
     if (h < nq) {
         weights_of(a.q_weight);
@@ -378,7 +414,7 @@ novakv_rotate_kernel(const __grid_constant__ RotateArgs a) {
             float x[8], y[8];
             unpack_unit(r.x, x);
             unpack_unit(r.y, y);
-            transform_row<D, IL>(a, norm, wx, wy, turn, x, y);
+            transform_row<D, IL>(a, turn, ka, kb, x, y);
             if (h + sub < a.hq) {
                 store_unit<VEC>(out + h * D + 8 * ka, pack_unit(x));
                 store_unit<VEC>(out + h * D + 8 * kb, pack_unit(y));
@@ -389,6 +425,7 @@ novakv_rotate_kernel(const __grid_constant__ RotateArgs a) {
     h -= nq;
     if (h < nk) {
         weights_of(a.k_weight);
+        const bool apart = D == 64 || IL || a.rot_dim == 0 || a.rot_dim == D;
 #pragma unroll 1
         for (; h < nk; h += step) {
             const Row r = next;
@@ -397,11 +434,11 @@ novakv_rotate_kernel(const __grid_constant__ RotateArgs a) {
             float x[8], y[8];
             unpack_unit(r.x, x);
             unpack_unit(r.y, y);
-            bool sure = transform_row<D, IL>(a, norm, wx, wy, turn, x, y);
+            bool sure = transform_row<D, IL>(a, turn, ka, kb, x, y);
             if constexpr (DST == DST_INT4) {
                 uint8_t* chunk = a.k_pages + ((size_t)page * a.hkv + h + sub) * I4Layout<D>::CHUNK_BYTES;
                 Quantised<D, true> code;
-                sure = code.template form<IL>(ka, kb, x, y) && sure;
+                sure = (apart ? code.template form<IL, true>(ka, kb, x, y) : code.template form<IL, false>(ka, kb, x, y)) && sure;
                 if (__any_sync(0xffffffffu, live && !sure)) store_row64<D, IL>(a, pos, l, ka, kb, r.x, r.y, chunk, live);
                 else if (live) code.store(chunk, slot, l, ka, kb);
             } else if (live) {
@@ -424,7 +461,7 @@ novakv_rotate_kernel(const __grid_constant__ RotateArgs a) {
             unpack_unit(r.x, x);
             unpack_unit(r.y, y);
             Quantised<D, false> code;
-            code.template form<false>(l, l + LANES, x, y);
+            code.template form<false, true>(l, l + LANES, x, y);
             if (live) code.store(a.v_pages + ((size_t)page * a.hkv + h + sub) * I4Layout<D>::CHUNK_BYTES, slot, l, l, l + LANES);
         } else if (live) {
             __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.v_pages) + (((size_t)page * a.hkv + h + sub) * NOVAKV_PAGE_TOKENS + slot) * D;
@@ -437,66 +474,95 @@ novakv_rotate_kernel(const __grid_constant__ RotateArgs a) {
 // Read-back of the 4-bit cache: a row belongs to D / 16 lanes, and what they store at a time lies side by side.
 struct GatherArgs {
     const int32_t *tok_seq, *tok_pos, *page_table;
-    int n_tokens, hkv, n_pages, max_pages_per_seq, n_seq;
+    int n_tokens, hkv, n_pages, max_pages_per_seq, n_seq, parts;     // parts: warps of a token
     const uint8_t *k_pages, *v_pages;
     void *k_out, *v_out;
     uint32_t* dev_status;
 };
 
+// Values of the code word of 8 channels, as four pairs of bf16: 128 + code is a bfloat16 number that one OR makes, 128 is taken off
+// exactly, and zero + scale code is rounded once.
+__device__ __forceinline__ uint4 word_values(uint32_t w, __nv_bfloat162 scale, __nv_bfloat162 zero) {
+    uint32_t v[4];                                                // channels (i, i + 4)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t c = (w >> (4 * i) & 0x000f000fu) | 0x43004300u;
+        const __nv_bfloat162 x = __hfma2(scale, __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&c), __float2bfloat162_rn(128.f)), zero);
+        v[i] = *reinterpret_cast<const uint32_t*>(&x);
+    }
+    return make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
+}
+
+// A warp takes the heads of a token, 2 x 32 / (D / 16) rows of keys and of values at a time.
 template <int D, bool FP32>
 __global__ void __launch_bounds__(ROT_THREADS)
 novakv_int4_gather_kernel(const GatherArgs a) {
     using Lay = I4Layout<D>;
-    constexpr int LANES = D / 16;
+    constexpr int LANES = D / 16, RPW = 32 / LANES, AT_ONCE = 2;
     novakv_grid_dependency_wait();
-    const long long row = ((long long)blockIdx.x * ROT_THREADS + threadIdx.x) / LANES;
-    const int l = threadIdx.x % LANES;
-    if (row >= (long long)a.n_tokens * a.hkv) return;
-    const int t = (int)(row / a.hkv), h = (int)(row - (long long)t * a.hkv);
+    const int lane = threadIdx.x & 31, sub = lane / LANES, l = lane % LANES;
+    const int warp = blockIdx.x * (ROT_THREADS / 32) + threadIdx.x / 32, t = warp / a.parts, part = warp - t * a.parts;
+    if (t >= a.n_tokens) return;
     const int seq = a.tok_seq[t], pos = a.tok_pos[t];
     if (seq == -1) return;
     if (seq < 0 || seq >= a.n_seq || pos < 0 || pos / NOVAKV_PAGE_TOKENS >= a.max_pages_per_seq) {
-        if (h == 0 && l == 0) atomicOr(a.dev_status, NOVAKV_DEV_BAD_TOKEN);
+        if (part == 0 && lane == 0) atomicOr(a.dev_status, NOVAKV_DEV_BAD_TOKEN);
         return;
     }
     const int page = a.page_table[(size_t)seq * a.max_pages_per_seq + pos / NOVAKV_PAGE_TOKENS];
     if (page < 0 || page >= a.n_pages) {
-        if (h == 0 && l == 0) atomicOr(a.dev_status, NOVAKV_DEV_BAD_PAGE);
+        if (part == 0 && lane == 0) atomicOr(a.dev_status, NOVAKV_DEV_BAD_PAGE);
         return;
     }
-    const size_t tile = ((size_t)page * a.hkv + h) * Lay::CHUNK_BYTES + (pos % NOVAKV_PAGE_TOKENS / I4_TILE) * Lay::TILE_BYTES;
     // 16 bytes of a row at a time: 8 channels of bf16 or 4 of binary32
     constexpr int CH = FP32 ? 4 : 8, N = D / (LANES * CH);
     const int slot = pos % I4_TILE;
-    uint32_t code[2][N], meta[2][Lay::GROUPS];
+    const size_t tile = (size_t)page * a.hkv * Lay::CHUNK_BYTES + (pos % NOVAKV_PAGE_TOKENS / I4_TILE) * Lay::TILE_BYTES;
+#pragma unroll 1
+    for (int h0 = part * AT_ONCE * RPW; h0 < a.hkv; h0 += a.parts * AT_ONCE * RPW) {
+        uint32_t code[AT_ONCE][2][N], meta[AT_ONCE][2][Lay::GROUPS];
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const uint8_t* src = (side ? a.v_pages : a.k_pages) + tile;
+        for (int e = 0; e < AT_ONCE; ++e) {
+            const int h = min(h0 + e * RPW + sub, a.hkv - 1);     // (rows behind the last head are read again, and not written)
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = (i * LANES + l) * CH;
-            const uint8_t* at = src + Lay::word(slot, c / 8) + c % 8 / 2;
-            code[side][i] = FP32 ? *reinterpret_cast<const uint16_t*>(at) : *reinterpret_cast<const uint32_t*>(at);
+            for (int side = 0; side < 2; ++side) {
+                const uint8_t* src = (side ? a.v_pages : a.k_pages) + tile + (size_t)h * Lay::CHUNK_BYTES;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int c = (i * LANES + l) * CH;
+                    const uint8_t* at = src + Lay::word(slot, c / 8) + c % 8 / 2;
+                    code[e][side][i] = FP32 ? *reinterpret_cast<const uint16_t*>(at) : *reinterpret_cast<const uint32_t*>(at);
+                }
+#pragma unroll
+                for (int g = 0; g < Lay::GROUPS; ++g) meta[e][side][g] = *reinterpret_cast<const uint32_t*>(src + Lay::pair(slot, g));
+            }
         }
 #pragma unroll
-        for (int g = 0; g < Lay::GROUPS; ++g) meta[side][g] = *reinterpret_cast<const uint32_t*>(src + Lay::pair(slot, g));
+        for (int e = 0; e < AT_ONCE; ++e) {
+            const int h = h0 + e * RPW + sub;
+            if (h >= a.hkv) break;
+#pragma unroll
+            for (int side = 0; side < 2; ++side)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int c = (i * LANES + l) * CH;
+                    const uint32_t m = Lay::GROUPS == 1 || c < I4_GROUP ? meta[e][side][0] : meta[e][side][Lay::GROUPS - 1];
+                    const size_t o = ((size_t)t * a.hkv + h) * D + c;
+                    if constexpr (FP32) {
+                        const float scale = __uint_as_float(m << 16), zero = __uint_as_float(m & 0xffff0000u);
+                        float x[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)               // (2^23 + code is a number that one OR makes)
+                            x[k] = fmaf(scale, __uint_as_float((code[e][side][i] >> (4 * k) & 15u) | 0x4b000000u) - 8388608.f, zero);
+                        *reinterpret_cast<float4*>(reinterpret_cast<float*>(side ? a.v_out : a.k_out) + o) = make_float4(x[0], x[1], x[2], x[3]);
+                    } else {
+                        const uint32_t s2 = __byte_perm(m, 0, 0x1010), z2 = __byte_perm(m, 0, 0x3232);
+                        *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(side ? a.v_out : a.k_out) + o) =
+                            word_values(code[e][side][i], *reinterpret_cast<const __nv_bfloat162*>(&s2), *reinterpret_cast<const __nv_bfloat162*>(&z2));
+                    }
+                }
+        }
     }
-#pragma unroll
-    for (int side = 0; side < 2; ++side)
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = (i * LANES + l) * CH;
-            const uint32_t m = Lay::GROUPS == 1 || c < I4_GROUP ? meta[side][0] : meta[side][Lay::GROUPS - 1];
-            const float scale = __uint_as_float(m << 16), zero = __uint_as_float(m & 0xffff0000u);
-            float x[CH];
-#pragma unroll
-            for (int k = 0; k < CH; ++k) x[k] = fmaf(scale, (float)(code[side][i] >> (4 * k) & 15u), zero);
-            const size_t o = (size_t)row * D + c;
-            if constexpr (FP32)
-                *reinterpret_cast<float4*>(reinterpret_cast<float*>(side ? a.v_out : a.k_out) + o) = make_float4(x[0], x[1], x[2], x[3]);
-            else
-                *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(side ? a.v_out : a.k_out) + o) = pack_unit(x);
-        }
 }
 
 template <int D, int DST, bool IL>
@@ -634,11 +700,12 @@ extern "C" novakv_status novakv_int4_gather(novakv_ctx* ctx, const int32_t* tok_
     if (((uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)k_out | (uintptr_t)v_out) & 15) return NOVAKV_EINVAL;
     if (((uintptr_t)tok_seq | (uintptr_t)tok_pos | (uintptr_t)page_table) & 3) return NOVAKV_EINVAL;
     const int d = ctx->cfg.head_dim;
-    const long long blocks = ((long long)n_tokens * ctx->cfg.n_kv_heads * (d / 16) + ROT_THREADS - 1) / ROT_THREADS;
-    if (blocks > 0x7fffffffll) return NOVAKV_ESHAPE;
+    const int rounds = (ctx->cfg.n_kv_heads + 1024 / d - 1) / (1024 / d);
+    const int parts = min(rounds, max(1, (64 * ctx->n_sm + n_tokens - 1) / n_tokens));
+    const long long blocks = ((long long)n_tokens * parts + ROT_THREADS / 32 - 1) / (ROT_THREADS / 32);
     const novakv_device_guard guard(ctx);
     if (!guard.ok) return NOVAKV_ECUDA;
-    const GatherArgs a = {tok_seq, tok_pos, page_table, n_tokens, ctx->cfg.n_kv_heads, n_pages, max_pages_per_seq, n_seq,
+    const GatherArgs a = {tok_seq, tok_pos, page_table, n_tokens, ctx->cfg.n_kv_heads, n_pages, max_pages_per_seq, n_seq, parts,
                           k_pages, v_pages, k_out, v_out, ctx->dev_status};
     auto* kern = d == 128 ? (out_is_fp32 ? novakv_int4_gather_kernel<128, true> : novakv_int4_gather_kernel<128, false>)
                           : (out_is_fp32 ? novakv_int4_gather_kernel<64, true> : novakv_int4_gather_kernel<64, false>);

@@ -124,6 +124,28 @@ def test_non_finite_rows_stay_in_their_head(contexts):
         check_rows(got[t:t + 1, h:h + 1], ref, size)
 
 
+@pytest.mark.parametrize("rot,interleaved", [(0, False), (32, False), (32, True)])
+def test_channels_that_do_not_turn_are_left_alone(contexts, rot, interleaved):
+    """Infinities and NaN in a channel behind the rotated ones reach no other channel."""
+    shape = (4, 2, 64)
+    ctx, gen = contexts(shape), np.random.default_rng(6)
+    tr, rq, _ = make_transform(gen, 64, False, rot, interleaved)
+    q = draw(gen, 4, 4, 64)
+    q[:, :, rot], q[:, :, 50], q[:, :, 63] = np.inf, np.nan, -np.inf
+    out = torch.empty((4, 4, 64), dtype=torch.bfloat16, device="cuda")
+    ctx.novakv_qk_norm_rope(tr, bf16(q), None, dev(np.arange(4, dtype=np.int32)), out, None)
+    got = host(out)
+    assert np.array_equal(got[..., rot:], q[..., rot:], equal_nan=True)
+    ref, size = R.transform(q[..., :max(rot, 1)], np.arange(4), **rq)
+    if rot:
+        check_rows(got[..., :rot], ref, size)
+    pools = [torch.zeros((1, 2, 64, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    seq, pos = dev(np.zeros(4, np.int32)), dev(np.arange(4, dtype=np.int32))
+    ctx.novakv_bf16_append(None, bf16(q[:, :2]), bf16(q[:, 2:]), seq, pos, *pools, dev(np.zeros((1, 1), np.int32)), torch.zeros(1, dtype=torch.int32, device="cuda"))
+    for pool, x in zip(pools, (q[:, :2], q[:, 2:])):
+        assert np.array_equal(host(pool)[0, :, :4].transpose(1, 0, 2), x, equal_nan=True)
+
+
 # ------------------------------------------------------------------------------------------------ appends
 def lists(gen, kind, n):
     """tok_seq, tok_pos of n entries over three sequences of up to 320 tokens."""
