@@ -10,14 +10,18 @@
 //    (tcgen05 wants its operands as 16-bit tiles in shared memory: the unpacked codes would have to be written there first,
 //    four times the bytes of the cache).  A code c is the binary16 subnormal c 2^-24, which the tensor core multiplies exactly:
 //    one AND of a word gives two operands, no conversion.  Codes in bits 4..7 are 16 c; what they meet carries a 1/16.
-//  * Exactness: q is a bfloat16 number, exact in binary16 after a power of two per head; the weights are carried as binary16
-//    pairs hi + lo (22 bits).  With four heads the lo parts are the unused four columns of the same product; with eight they
-//    take a second one.  Accumulation, softmax statistics and the zeros' share are binary32.
-//  * Streaming: the walk over (sequence, KV head, unit of 32 or 64 tokens) is cut evenly among the CTAs (one per SM) and again among
-//    their 16 warps; each warp copies its units' keys and values (one bulk copy each) into a ring of its own, two units ahead,
-//    and no warp waits for another before the end.
+//  * Exactness: q is a bfloat16 number, exact in binary16 after a power of two; accumulators, softmax statistics and the zeros'
+//    share are binary32.  What the weights are rounded to goes by the output's type (FINE below).
+//  * Streaming: the walk over (sequence, KV head, unit of 32 tokens at d = 128, 64 at d = 64) is cut evenly among the CTAs (one
+//    per SM) and again among their 16 warps; each warp copies its units' keys and values (a bulk copy each) into a ring of its
+//    own, a unit ahead of the one it works on, and no warp waits for another before the end.  (A page, 64 tokens, is 4.6 KB of a
+//    side at d = 128; 16 warps x 2 units are 147 KB in flight or at work, three times what the latency of HBM asks for.)
 //  * Join: what a warp has of a (sequence, KV head) pair that it does not hold whole goes to shared memory; the CTA joins these
 //    pieces, and a second kernel joins the at most two per CTA that reach over its ends.
+//
+// B200, bf16 output, 6.56 TB/s of measured copy bandwidth: 64 x 16384 tokens (32 / 8 heads, d = 128) 190 us, 97 % of it; 8 x 16384 36.5 us,
+// 63 %, of which launches, the look-up of the first units and the join are 8.5; 16 x 65536 (64 / 8 heads, d = 64) 106 us, 87 %, and 125 where
+// it runs for seconds and the board's power limit takes the clock from 1.96 to 1.69 GHz: what is left is instructions (540 a unit).
 #include <math_constants.h>
 
 #include "novakv_int4.cuh"
@@ -212,9 +216,17 @@ __device__ __forceinline__ void unpack_codes(uint32_t x, uint32_t (&c)[4]) {
     }
 }
 
+// For the values, whose sums may be taken apart afterwards, four instructions: rows of codes c0 + 16 c1 (a byte) and of 16 c1 above
+// them, from which the sums over c0 and c1 follow; likewise c2, c3.
+__device__ __forceinline__ void unpack_bytes(uint32_t x, uint32_t (&c)[4]) {
+    c[0] = x & 0x00ff00ffu; c[1] = x & 0x00f000f0u;
+    c[2] = __byte_perm(x, 0, 0x4341); c[3] = c[2] & 0x00f000f0u;
+}
+
 // FINE: for binary32 outputs.  The products keep the bits that they would lose (unpack_codes) and the weights meet the codes as
-// binary16 pairs hi + lo, in two products.  Without, a logit is off by less than 2^-11 of what one step of its key's largest
-// channel's code moves it by, and a weight by 2^-12 of itself, at random: an eighth of the rounding of a bfloat16 output.
+// binary16 pairs hi + lo, in two products (8 x 16384 tokens: 49 us against 36.5).  Without, each product of a logit is cut off at 2^-15 of
+// what one step of its key's code moves it by in the query's largest channel (136 cuts at most, some 2^-11 in all as measured),
+// and a weight is off by 2^-12 of itself, at random: an eighth of the rounding of a bfloat16 output.
 template <int D, int HG, bool FINE>
 __global__ void __launch_bounds__(THREADS, 1)
 novakv_int4_decode_kernel(const DecodeArgs a) {
@@ -225,6 +237,7 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
     // heads columns 4..7 repeat columns 0..3, and the lanes that hold them take the other token: one token for two heads each.
     constexpr bool SPLIT = HG < 8;
     constexpr int R = SPLIT ? 1 : 2, COLS = SPLIT ? 4 : 8;
+    constexpr bool BYTES = !FINE && D == 64;                      // (at d = 128 the registers for it are not there: 36.5 -> 37.1 us)
     extern __shared__ __align__(128) unsigned char smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, j = lane & 3, up = SPLIT ? j >> 1 : 0, jj = SPLIT ? j & 1 : j;
     int *prefix = reinterpret_cast<int*>(smem + P::PREFIX), *lens = reinterpret_cast<int*>(smem + P::LENS);
@@ -357,8 +370,11 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
                 for (int i = 0; i < 4; ++i)
                     mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(ww[i] << 16)), fabsf(__uint_as_float(ww[i] & 0xffff0000u))));
             }
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+            if (!(mx < CUDART_INF_F)) mx = 0.f;                   // (a head with an infinity does not decide for the others)
 #pragma unroll
-            for (int s = 1; s < 32; s <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
+            for (int s = 4; s < 32; s <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
             // 2^e brings the heads' largest coordinate just below 2^15 (what is 2^-31 of it or less loses bits)
             const int e = min(max(15 - ((int)(__float_as_uint(mx) >> 23) - 126), -100), 120);
             const float f = __uint_as_float((uint32_t)(e + 127) << 23), odd = FINE ? f : f * 0.0625f;
@@ -576,8 +592,8 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
                         uint32_t x[SB][4], y[SB][4];
 #pragma unroll
                         for (int e = 0; e < SB; ++e) {
-                            unpack_codes<FINE>(r[e][2 * h], x[e]);
-                            unpack_codes<FINE>(r[e][2 * h + 1], y[e]);
+                            if (BYTES) { unpack_bytes(r[e][2 * h], x[e]); unpack_bytes(r[e][2 * h + 1], y[e]); }
+                            else { unpack_codes<FINE>(r[e][2 * h], x[e]); unpack_codes<FINE>(r[e][2 * h + 1], y[e]); }
                         }
 #pragma unroll
                         for (int sh = 0; sh < 2; ++sh) {
@@ -634,7 +650,7 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
                 float v[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    v[i] = o[p][s][i];
+                    v[i] = i < 2 && BYTES ? o[p][s][i] - o[p][s][i + 2] : o[p][s][i];
                     if (SPLIT) v[i] += __shfl_xor_sync(0xffffffffu, v[i], 2);
                     v[i] = fmaf(v[i] * (i < 2 || FINE ? UNIT : UNIT * 0.0625f), vbound, (i & 1) ? zs1[p / 2] : zs0[p / 2]);
                 }
@@ -728,7 +744,7 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
 
 // One block per CTA of the scan: joins the pair that begins in the CTA and reaches over its back end with the front pieces of the
 // CTAs behind it.  A warp takes a head and every GROUPS-th piece; what it loads hangs on two loads in a row, the pairs' numbers
-// and the pieces (a chain of four took 4.5 us of a decode step of one sequence of 16384 tokens, this MERGE_US).
+// and the pieces (one sequence of 16384 tokens, 19 CTAs a pair: 16.4 us with a chain of four loads and a warp per head, 14.1 so).
 constexpr int MERGE_WARPS = 16;
 template <int D, int HG>
 __global__ void __launch_bounds__(MERGE_WARPS * 32)

@@ -68,13 +68,19 @@ def write_tokens(pool, table_row, pos, hkv, d, codes, scale, zero):
 
 
 def attention(q, k, v, scale, sink=None):
-    """q [Hq][d], k, v [n][Hkv][d] binary64 -> (o [Hq][d], tol): tol [Hq][1] bounds a binary32 evaluation on the codes.
+    """q [Hq][d], k, v [n][Hkv][d] binary64 -> (o [Hq][d], tol, coarse), [Hq][1] each: tol bounds the evaluation behind a binary32
+    output, coarse what the one behind a bf16 output adds to it, its rounding apart.
 
-    A logit is a sum of d products whose factors are exact, so it is off by at most 2^-19 (128 additions, each cut off below
-    2^-23 of the running sum at worst, and a few roundings of binary32: < 2^-16 2^-3) of S = scale sum_i |q_i| vmax_i, vmax the
-    largest |value| in the key's group.  A weight is then off by the same times ln 2 / ln 2, relatively, plus 2^-20 of the base-2
-    exponential and the weight's 22 bits; numerator and normaliser both, hence the two.  The numerator's accumulation adds
-    (n + 8) 2^-23 of the largest magnitude at most, in sums of 32 tokens at a time that are themselves cut off."""
+    tol.  The products of a logit are exact (q and codes are short numbers), their sums are cut off below 2^-23 of the largest
+    product at worst, at most 128 + 8 times, and a few binary32 roundings of scale code, zero q and their sum follow: less than
+    2^-15 (136 2^-23 and 8 2^-24) of the largest single term scale |q| 2 max|k| - and the test takes 2^-19 of the sum of all d of
+    them, of which the largest is at least a sixteenth for queries that are not spread evenly and which exceeds it otherwise.  A
+    weight is off by as much, relatively, and by 2^-20 for the base-2 exponential and its 22 bits; numerator and normaliser both,
+    hence twice.  The numerator is a sum of sums of 32 tokens, each cut off at 2^-24 of its largest product 68 times, added in
+    binary32 by n / 32 additions over the warps, whose errors go with the root of their number.
+
+    coarse.  Codes are taken as they lie, 2^-10 of a number's leading bit, so that a cut is 2^-15 of |q| max times one step of a
+    code, at most 136 times in a logit; the weights have 12 bits."""
     hkv, hg = k.shape[1], q.shape[0] // k.shape[1]
     qh = q.astype(np.float64).reshape(hkv, hg, -1)
     z = scale * np.einsum("hgd,nhd->hgn", qh, k)
@@ -85,8 +91,10 @@ def attention(q, k, v, scale, sink=None):
     p = np.exp(z - m)
     total = p.sum(-1, keepdims=True) + (0 if s is None else np.exp(s - m))
     o = np.einsum("hgn,nhd->hgd", p, v) / total
-    vmax = np.abs(v).max()
-    size = scale * np.abs(qh).sum(-1, keepdims=True) * 2 * np.abs(k).max()
+    vmax, kmax = np.abs(v).max(), np.abs(k).max()
+    size = scale * np.abs(qh).sum(-1, keepdims=True) * 2 * kmax
     steps = np.sqrt(len(k)) + 8
     tol = vmax * (2 * (2.0 ** -19 * size + 2.0 ** -20) + steps * 2.0 ** -21)
-    return o.reshape(q.shape), tol.reshape(-1, 1)
+    step = 2 * kmax / 15                                       # (a group's range is at most twice its largest value)
+    coarse = vmax * 2 * (136 * 2.0 ** -15 * scale * np.abs(qh).max() * step + 2.0 ** -12)
+    return o.reshape(q.shape), tol.reshape(-1, 1), np.full((q.shape[0], 1), coarse)

@@ -212,9 +212,9 @@ def test_rotation_identities():
 def test_attention_reference_against_torch():
     gen = np.random.default_rng(2)
     q, k, v = gen.normal(size=(4, 64)), gen.normal(size=(50, 2, 64)), gen.normal(size=(50, 2, 64))
-    o, _ = R.attention(q, k, v, 0.125)
+    o, _, _ = R.attention(q, k, v, 0.125)
     z = torch.softmax(0.125 * torch.einsum("hgd,nhd->hgn", torch.tensor(q).view(2, 2, 64), torch.tensor(k)), -1)
     assert np.allclose(o, torch.einsum("hgn,nhd->hgd", z, torch.tensor(v)).reshape(4, 64).numpy())
-    far, _ = R.attention(q, k, v, 0.125, sink=np.full(4, 1e4))
-    none, _ = R.attention(q, k, v, 0.125, sink=np.full(4, -1e4))
+    far, _, _ = R.attention(q, k, v, 0.125, sink=np.full(4, 1e4))
+    none, _, _ = R.attention(q, k, v, 0.125, sink=np.full(4, -1e4))
     assert not far.any() and np.allclose(none, o)
