@@ -63,7 +63,7 @@ struct DecodeArgs {
     const uint8_t *k_pages, *v_pages;
     int n_pages;
     const int32_t *page_table, *seq_lens;
-    int max_pages_per_seq, batch, hkv, window, out_is_fp32, one;   // one: a CTA for each pair, which joins all of it
+    int max_pages_per_seq, batch, hkv, window, out_is_fp32, one, few;   // one: a CTA for each pair, which joins all of it; few: at most 32 sequences, the cost fits 32 bits
     float scale_log2;
     const float* sink;
     void* out;
@@ -127,66 +127,50 @@ __device__ __forceinline__ Sight sight_of(const DecodeArgs& a, int len) {
 }
 // Where a unit of the walk lies: sequence, KV head, unit of the pair.
 struct Place { int b, kvh, unit; Sight s; };
-// The walk over all pairs: prefix[i] units (of one KV head) and seqs[i] sequences with a token lie before sequence i chunk.
+// The walk over all pairs: prefix[i] units (of one KV head) and seqs[i] sequences with a token lie before sequence i chunk.  It is
+// cut where the cost is even: units, and PAIR_COST in front of each pair.
 struct Walk {
     const int *prefix, *seqs, *lens;
     int chunk;
     __device__ __forceinline__ int len(const DecodeArgs& a, int b) const { return chunk == 1 ? lens[b] : a.seq_lens[b]; }
-    template <int TOKENS>
-    __device__ __forceinline__ Place place(const DecodeArgs& a, int i, long long u) const {     // u lies behind prefix[i], before prefix[i + 1]
-        Place p;
-        p.b = i * chunk;
-        long long r = u - (long long)prefix[i] * a.hkv;
-        p.s = sight_of<TOKENS>(a, len(a, p.b));
-#pragma unroll 1
-        while (r >= (long long)p.s.units * a.hkv && p.b + 1 < a.batch) {
-            r -= (long long)p.s.units * a.hkv;
-            p.s = sight_of<TOKENS>(a, len(a, ++p.b));
-        }
-        const int units = max(p.s.units, 1);
-        p.kvh = min((int)r / units, a.hkv - 1);
-        p.unit = (int)r - p.kvh * units;
-        return p;
-    }
-    // by one thread
-    template <int TOKENS>
-    __device__ __forceinline__ Place find(const DecodeArgs& a, long long u) const {
-        int lo = 0, hi = THREADS;                                 // prefix[lo] hkv <= u < prefix[hi] hkv
-#pragma unroll 1
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if ((long long)prefix[mid] * a.hkv <= u) lo = mid;
-            else hi = mid;
-        }
-        return place<TOKENS>(a, lo, u);
-    }
-    // The walk is cut where the cost - units, and PAIR_COST for each pair - is even.  Units before cost x, by a warp.
     __device__ __forceinline__ long long cost(const DecodeArgs& a, int i) const { return (prefix[i] + (long long)PAIR_COST * seqs[i]) * a.hkv; }
+    // A sequence that is met on the way: cost and units before it.
+    struct Stop { long long cost, units; int b; Sight s; };
+    // The sequence in which cost x lies (x < the total), by a warp: 32 entries, then the 16 between two of them, then one by one.
     template <int TOKENS>
-    __device__ __forceinline__ long long units_before(const DecodeArgs& a, long long x, int lane) const {
+    __device__ __forceinline__ Stop find(const DecodeArgs& a, long long x, int lane) const {
         constexpr int STEP = THREADS / 32;
         int i = (31 - __clz(__ballot_sync(0xffffffffu, cost(a, lane * STEP) <= x))) * STEP;
         i += 31 - __clz(__ballot_sync(0xffffffffu, lane < STEP && cost(a, i + lane % STEP) <= x));
-        long long left = x - cost(a, i), units = (long long)prefix[i] * a.hkv;
-        for (int b = i * chunk; b < min(a.batch, (i + 1) * chunk); ++b) {
-            const int n = sight_of<TOKENS>(a, len(a, b)).units;
-            if (n == 0) continue;
-            if (left < (long long)(n + PAIR_COST) * a.hkv) {
-                const int pair = (int)(left / (n + PAIR_COST));
-                return units + (long long)pair * n + max((int)(left - (long long)pair * (n + PAIR_COST)) - PAIR_COST, 0);
-            }
-            left -= (long long)(n + PAIR_COST) * a.hkv;
-            units += (long long)n * a.hkv;
+        Stop w = {cost(a, i), (long long)prefix[i] * a.hkv, i * chunk, {}};
+        for (;; ++w.b) {
+            w.s = sight_of<TOKENS>(a, len(a, w.b));
+            const long long own = w.s.units > 0 ? (long long)(w.s.units + PAIR_COST) * a.hkv : 0;
+            if (x < w.cost + own || w.b + 1 >= a.batch) return w;
+            w.cost += own;
+            w.units += (long long)w.s.units * a.hkv;
         }
-        return units;
     }
-    // by a warp, for all of its lanes: 32 entries, then the 16 between two of them
+    // The first unit that is not before cost x, in the sequence where x lies; the units of the whole walk before it.
+    __device__ __forceinline__ long long enter(const Stop& w, long long x, Place& p) const {
+        const unsigned left = (unsigned)(x - w.cost), per = w.s.units + PAIR_COST, pair = left / per;
+        p.b = w.b;
+        p.s = w.s;
+        p.kvh = (int)pair;
+        p.unit = max((int)(left - pair * per) - PAIR_COST, 0);
+        return w.units + (long long)pair * w.s.units + p.unit;
+    }
+    // to the pair that a unit counted from this one's first lies in
     template <int TOKENS>
-    __device__ __forceinline__ Place find_warp(const DecodeArgs& a, long long u, int lane) const {
-        constexpr int STEP = THREADS / 32;
-        const int i = 31 - __clz(__ballot_sync(0xffffffffu, (long long)prefix[lane * STEP] * a.hkv <= u));
-        const int k = 31 - __clz(__ballot_sync(0xffffffffu, lane < STEP && (long long)prefix[i * STEP + lane % STEP] * a.hkv <= u));
-        return place<TOKENS>(a, i * STEP + k, u);
+    __device__ __forceinline__ void settle(const DecodeArgs& a, Place& p) const {
+#pragma unroll 1
+        while (p.unit >= p.s.units) {
+            p.unit -= p.s.units;
+            if (++p.kvh < a.hkv) continue;
+            p.kvh = 0;
+            do p.s = sight_of<TOKENS>(a, len(a, ++p.b));
+            while (p.s.units == 0 && p.b + 1 < a.batch);
+        }
     }
 };
 
@@ -255,9 +239,8 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
 
     // ---- the walk over (sequence, KV head, unit), and this warp's share of it
     int* seqs = reinterpret_cast<int*>(smem + P::SEQS);
-    const Walk walk = {prefix, seqs, lens, (a.batch + THREADS - 1) / THREADS};
+    const Walk walk = {prefix, seqs, a.few ? a.seq_lens : lens, (a.batch + THREADS - 1) / THREADS};
     Place at = {};                                                // the warp's first unit
-    long long first = 0;
     int n = 0;
     bool idle = false;                                            // some sequence has no token
     if (a.one) {
@@ -269,6 +252,43 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
         at.unit = at.s.units * warp / WARPS;
         n = at.s.units * (warp + 1) / WARPS - at.unit;
         idle = at.s.units == 0;
+        __syncthreads();
+    } else if (a.few) {
+        // Up to 32 sequences, a lane each: every warp forms the walk itself, and nothing of it waits for another.  (3000 cycles
+        // to a warp's first unit where the general way below takes 4600: code that runs once runs at the pace of its fetches.)
+        const int len = lane < a.batch ? a.seq_lens[lane] : 0;
+        if (blockIdx.x == 0 && warp == 0 && len > a.max_pages_per_seq * NOVAKV_PAGE_TOKENS) atomicOr(a.dev_status, NOVAKV_DEV_BAD_LENGTH);
+        const int units = sight_of<P::TOKENS>(a, len).units, own = units > 0 ? (units + PAIR_COST) * a.hkv : 0;
+        int cost = own, before = units;
+#pragma unroll 1
+        for (int s = 1; s < 32; s <<= 1) {
+            const int c = __shfl_up_sync(0xffffffffu, cost, s), u = __shfl_up_sync(0xffffffffu, before, s);
+            if (lane >= s) { cost += c; before += u; }
+        }
+        const unsigned total = __shfl_sync(0xffffffffu, cost, 31), all = __shfl_sync(0xffffffffu, before, 31) * a.hkv;
+        cost -= own;
+        before = (before - units) * a.hkv;
+        idle = __any_sync(0xffffffffu, lane < a.batch && units == 0);
+        const unsigned ctas = max(1u, min(gridDim.x, total / (PAIR_COST + 1))), cta = min(blockIdx.x, ctas), each = total / ctas, more = total - each * ctas;
+        const unsigned c0 = each * cta + min(cta, more), share = cta < ctas ? each + (cta < more) : 0;
+        const unsigned x[2] = {c0 + (share * warp >> 4), c0 + (share * (warp + 1) >> 4)};
+        unsigned units_at[2] = {all, all};
+        if (x[0] < x[1]) {
+#pragma unroll 1
+            for (int e = 1; e >= 0; --e) {
+                const unsigned xe = e ? x[1] : x[0];
+                if (xe >= total) continue;
+                const int b = 31 - __clz(__ballot_sync(0xffffffffu, own > 0 && (unsigned)cost <= xe));
+                at.b = b;
+                at.s = sight_of<P::TOKENS>(a, __shfl_sync(0xffffffffu, len, b));
+                const unsigned left = xe - __shfl_sync(0xffffffffu, cost, b), per = at.s.units + PAIR_COST;
+                at.kvh = left / per;
+                at.unit = max((int)(left - at.kvh * per) - PAIR_COST, 0);
+                const unsigned u = __shfl_sync(0xffffffffu, before, b) + at.kvh * at.s.units + at.unit;
+                if (e) units_at[1] = u; else units_at[0] = u;
+            }
+            n = units_at[1] - units_at[0];
+        }
         __syncthreads();
     } else {
         int sum = 0, used = 0;
@@ -300,11 +320,23 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
         idle = __syncthreads_or(idle);
         const long long total = walk.cost(a, THREADS);
         // (no CTA in between without a unit, since the join goes by the CTAs' order: a CTA takes more cost than a pair's own)
-        const long long ctas = max(1ll, min((long long)gridDim.x, total / (PAIR_COST + 1))), cta = min((long long)blockIdx.x, ctas);
-        const long long c0 = total * cta / ctas, c1 = total * min(cta + 1, ctas) / ctas;
-        first = walk.units_before<P::TOKENS>(a, c0 + (c1 - c0) * warp / WARPS, lane);
-        n = (int)(walk.units_before<P::TOKENS>(a, c0 + (c1 - c0) * (warp + 1) / WARPS, lane) - first);
-        if (n > 0) at = walk.find_warp<P::TOKENS>(a, first, lane);
+        const unsigned ctas = (unsigned)max(1ll, min((long long)gridDim.x, total / (PAIR_COST + 1))), cta = min(blockIdx.x, ctas);
+        const long long each = total >> 32 ? total / ctas : (long long)((unsigned)total / ctas);
+        const unsigned more = (unsigned)(total - each * ctas);    // (the first so many take one more)
+        const long long c0 = each * cta + min(cta, more), c1 = cta < ctas ? each * (cta + 1) + min(cta + 1, more) : c0;
+        const long long x0 = c0 + ((c1 - c0) * warp >> 4), x1 = c0 + ((c1 - c0) * (warp + 1) >> 4);
+        static_assert(WARPS == 16, "a sixteenth of a CTA's share");
+        if (x0 < x1) {
+            auto stop = walk.find<P::TOKENS>(a, x0, lane);
+            const long long first = walk.enter(stop, x0, at);
+            long long behind = (long long)prefix[THREADS] * a.hkv;
+            if (x1 < total) {
+                if (x1 >= stop.cost + (long long)(stop.s.units + PAIR_COST) * a.hkv) stop = walk.find<P::TOKENS>(a, x1, lane);
+                Place unused;
+                behind = walk.enter(stop, x1, unused);
+            }
+            n = (int)(behind - first);
+        }
     }
 
     // ---- producer: the units' chunks 32 at a time, the next batch always on its way
@@ -313,7 +345,7 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
         if (i >= n) return 0;
         Place p = begin;
         p.unit += i;
-        if (p.unit >= p.s.units) p = walk.find<P::TOKENS>(a, first + i);
+        walk.settle<P::TOKENS>(a, p);
         const int unit = p.s.t0 + p.unit;
         int page = a.page_table[(size_t)p.b * a.max_pages_per_seq + unit * P::TOKENS / NOVAKV_PAGE_TOKENS];
         if (page < 0 || page >= a.n_pages) {
@@ -720,12 +752,20 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
             float acc[D / 32];
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) acc[i] = 0.f;
-            for (uint32_t left = pieces; left; left &= left - 1) {
-                const int k = __ffs(left) - 1;
-                const float fk = __shfl_sync(0xffffffffu, f, k);
-                const float* src = piece(k) + 4 + lane * (D / 32);
+#pragma unroll 1
+            for (int k0 = 0; k0 < 2 * WARPS; k0 += 8) {           // eight slots' loads in flight together
+                if (!(pieces >> k0 & 255u)) continue;
+                float v[8][D / 32];
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) acc[i] = fmaf(fk, src[i], acc[i]);
+                for (int e = 0; e < 8; ++e)
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) v[e][i] = pieces >> (k0 + e) & 1 ? piece(k0 + e)[4 + lane * (D / 32) + i] : 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float fk = __shfl_sync(0xffffffffu, f, k0 + e);
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) acc[i] = fmaf(fk, v[e][i], acc[i]);
+                }
             }
             if (begins && ends) {
                 const float inv = 1.f / (l + sink_mass(a, pair % a.hkv * HG + h, m));
@@ -845,6 +885,7 @@ novakv_status launch_t(novakv_ctx* ctx, DecodeArgs& a, void* workspace, cudaStre
     const int seen = a.window > 0 ? min(a.window / P::TOKENS + 2, a.max_pages_per_seq * (NOVAKV_PAGE_TOKENS / P::TOKENS))
                                   : a.max_pages_per_seq * (NOVAKV_PAGE_TOKENS / P::TOKENS);
     a.one = pairs <= scan_ctas(ctx) && seen <= ONE_UNITS * WARPS;
+    a.few = !a.one && a.batch <= 32 && pairs * ((long long)a.max_pages_per_seq * (NOVAKV_PAGE_TOKENS / P::TOKENS) + PAIR_COST) < (1ll << 27);
     const dim3 grid(a.one ? (int)pairs : scan_ctas(ctx));
     if (novakv_launch_pdl(kern, grid, dim3(THREADS), P::TOTAL, stream, a) != cudaSuccess) return NOVAKV_ECUDA;
     ctx->launches++;
