@@ -79,6 +79,18 @@ __device__ __forceinline__ uint4 pack_unit(const T (&x)[8]) {
     return make_uint4(pack2((float)x[0], (float)x[1]), pack2((float)x[2], (float)x[3]), pack2((float)x[4], (float)x[5]),
                       pack2((float)x[6], (float)x[7]));
 }
+// two binary32 numbers side by side: one instruction does both (the append is bound by their number)
+struct Two {
+    uint64_t v;
+    __device__ __forceinline__ Two() = default;
+    __device__ __forceinline__ Two(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi)); }
+    __device__ __forceinline__ void get(float& lo, float& hi) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+};
+__device__ __forceinline__ Two operator+(Two a, Two b) { Two d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v)); return d; }
+__device__ __forceinline__ Two operator-(Two a, Two b) { Two d; asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v)); return d; }
+__device__ __forceinline__ Two operator*(Two a, Two b) { Two d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v)); return d; }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) { Two d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return d; }
+
 // minimum and maximum that keep a NaN: a group that holds one gets it as its zero
 __device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
@@ -101,22 +113,58 @@ __device__ __forceinline__ float& first_of(int i, float (&x)[8], float (&y)[8]) 
 template <bool IL>
 __device__ __forceinline__ float& second_of(int i, float (&x)[8], float (&y)[8]) { return !IL ? y[i] : i < 4 ? x[2 * i + 1] : y[2 * i - 7]; }
 
-// norm and rotation of a row's two units.  All lanes of the warp take part.  False where the sum of squares leaves the range in
-// which its roundings are relative ones.
-template <int D, bool IL>
+// norm and rotation of a row's two units.  All lanes of the warp take part.  False (PACKED alone) where the sum of squares leaves
+// the range in which its roundings are relative ones.
+// PACKED: two numbers an instruction, for the kernel that is bound by instructions; where memory is the bound its registers cost
+// more than it saves (16384 tokens, d = 64: 51.4 against 53.8 us).
+template <int D, bool IL, bool PACKED>
 __device__ __forceinline__ bool transform_row(const RotateArgs& a, const Turn& turn, int ua, int ub, float (&x)[8], float (&y)[8]) {
     constexpr int LANES = D / 16;
     bool fine = true;
-    if (turn.norm) {
-        float ss = 0.f, st = 0.f;
+    if constexpr (PACKED) {
+        Two p[4], q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { p[i] = Two(x[2 * i], x[2 * i + 1]); q[i] = Two(y[2 * i], y[2 * i + 1]); }
+        if (turn.norm) {
+            Two s0(0.f, 0.f), s1(0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { s0 = fma2(p[i], p[i], s0); s1 = fma2(q[i], q[i], s1); }
+            float ss, st;
+            (s0 + s1).get(ss, st);
+            ss += st;
+#pragma unroll
+            for (int s = 1; s < LANES; s <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
+            const float r = rsqrtf(fmaf(ss, 1.f / D, a.eps));
+            fine = ss > 1e-30f && ss < 1e30f;
+            const Two rr(r, r);
+            float w[8];
+            unpack_unit(turn.wx, w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = p[i] * (rr * Two(w[2 * i], w[2 * i + 1]));
+            unpack_unit(turn.wy, w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = q[i] * (rr * Two(w[2 * i], w[2 * i + 1]));
+        }
+        // (what is not rotated is left alone: infinity times 0 would be NaN)
+        if (!IL && 8 * ua < a.rot_dim) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const Two c(turn.c[2 * i], turn.c[2 * i + 1]), s(turn.s[2 * i], turn.s[2 * i + 1]);
+                const Two u = p[i] * c - q[i] * s;
+                q[i] = fma2(p[i], s, q[i] * c);
+                p[i] = u;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { p[i].get(x[2 * i], x[2 * i + 1]); q[i].get(y[2 * i], y[2 * i + 1]); }
+    } else if (turn.norm) {
+        float ss = 0.f, st = 0.f, w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) { ss = fmaf(x[i], x[i], ss); st = fmaf(y[i], y[i], st); }
         ss += st;
 #pragma unroll
         for (int s = 1; s < LANES; s <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
         const float r = rsqrtf(fmaf(ss, 1.f / D, a.eps));
-        fine = ss > 1e-30f && ss < 1e30f;
-        float w[8];
         unpack_unit(turn.wx, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] *= r * w[i];
@@ -124,13 +172,15 @@ __device__ __forceinline__ bool transform_row(const RotateArgs& a, const Turn& t
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] *= r * w[i];
     }
+    if (IL || !PACKED) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {                                 // (what is not rotated is left alone: infinity times 0 would be NaN)
-        if (8 * (IL && i >= 4 ? ub : ua) >= a.rot_dim) continue;
-        float &p = first_of<IL>(i, x, y), &q = second_of<IL>(i, x, y);
-        const float u = p * turn.c[i] - q * turn.s[i];
-        q = q * turn.c[i] + p * turn.s[i];
-        p = u;
+        for (int i = 0; i < 8; ++i) {
+            if (8 * (IL && i >= 4 ? ub : ua) >= a.rot_dim) continue;
+            float &e = first_of<IL>(i, x, y), &f = second_of<IL>(i, x, y);
+            const float u = e * turn.c[i] - f * turn.s[i];
+            f = f * turn.c[i] + e * turn.s[i];
+            e = u;
+        }
     }
     return fine;
 }
@@ -140,9 +190,9 @@ __device__ __forceinline__ bool transform_row(const RotateArgs& a, const Turn& t
 struct Divisor {
     float s, r;
     __device__ __forceinline__ explicit Divisor(float scale) : s(scale), r(1.f / scale) {}
-    __device__ __forceinline__ float quotient(float x) const {
-        const float q0 = x * r;
-        return fmaf(fmaf(-q0, s, x), r, q0);
+    __device__ __forceinline__ Two quotient(Two x) const {
+        const Two rr(r, r), q0 = x * rr;
+        return fma2(fma2(q0, Two(-s, -s), x), rr, q0);
     }
 };
 constexpr float ROUND = 12582912.f;          // 1.5 2^23: added and taken away again it leaves the nearest integer, ties to even
@@ -150,11 +200,11 @@ constexpr float ROUND = 12582912.f;          // 1.5 2^23: added and taken away a
 // Codes and pairs of a row.  All lanes of the warp take part.
 // A value row is given exactly.  A key (KEY) is defined by binary64, but formed in binary32 first: each element is off by less
 // than 2^-19 (|a| + |b|) of the pair it comes from (a mean of D squares and its root 14 roundings of 2^-24, cos and sin 5, far
-// positions 4, their products with weight, element and root 3, a sum 1: less than 32), which is at most sqrt(2) times that of the
+// positions 4, the root's product with weight and element 2, two products and a sum 3: less than 32), which is at most sqrt(2) times that of the
 // pair it gives.  Where no element, minimum or maximum can have crossed a border of its rounding by that, codes and pairs are
 // those of the binary64 key; else the answer is false, and the row is formed again in binary64: 0.9 % of the rows, 3 % of the
-// warps' four.  (In binary64 throughout, a prompt of 16384 tokens and 32 / 8 heads of d = 128 took 158 us where this takes 94;
-// its floor is 57, what bounds it is instructions: 2400 a token for keys and values, 1700 for the queries.)
+// warps' four.  (In binary64 throughout, a prompt of 16384 tokens and 32 / 8 heads of d = 128 took 158 us where this takes 91;
+// its floor is 57, what bounds it is instructions: 3700 a token, some 1400 of them for the queries.)
 template <int D, bool KEY>
 struct Quantised {
     uint32_t wx, wy;
@@ -177,8 +227,12 @@ struct Quantised {
             for (int i = 0; i < 8; ++i) {
                 dx[i] = OFF * (fabsf(x[i]) + fabsf(INTERLEAVED ? x[i ^ 1] : y[i]));
                 dy[i] = INTERLEAVED ? OFF * (fabsf(y[i]) + fabsf(y[i ^ 1])) : dx[i];
-                ux[i] = x[i] + dx[i]; uy[i] = y[i] + dy[i];
-                lx[i] = x[i] - dx[i]; ly[i] = y[i] - dy[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const Two x2(x[i], x[i + 1]), y2(y[i], y[i + 1]), dx2(dx[i], dx[i + 1]), dy2(dy[i], dy[i + 1]);
+                (x2 + dx2).get(ux[i], ux[i + 1]); (y2 + dy2).get(uy[i], uy[i + 1]);
+                (x2 - dx2).get(lx[i], lx[i + 1]); (y2 - dy2).get(ly[i], ly[i + 1]);
             }
             extremes(ux, xl, xh); extremes(uy, yl, yh);
             extremes(lx, xl2, xh2); extremes(ly, yl2, yh2);
@@ -229,12 +283,12 @@ struct Quantised {
         }
         return true;
     }
-    // four codes as a number of 16 bits, twice
+    // eight codes, given as -code: four as a number of 16 bits, twice
     static __device__ __forceinline__ uint32_t pack_codes(const float (&c)[8]) {
         float half[2];
 #pragma unroll
         for (int i = 7; i >= 0; --i) half[i / 4] = i % 4 == 3 ? c[i] : fmaf(half[i / 4], 16.f, c[i]);
-        return __byte_perm(__float_as_uint(half[0] + 8388608.f), __float_as_uint(half[1] + 8388608.f), 0x5410);
+        return __byte_perm(__float_as_uint(8388608.f - half[0]), __float_as_uint(8388608.f - half[1]), 0x5410);
     }
     static __device__ __forceinline__ void extremes(const float (&x)[8], float& lo, float& hi) {
         lo = min_nan(min_nan(x[0], x[1], x[2]), min_nan(x[3], x[4], x[5]), min_nan(x[6], x[7]));
@@ -242,10 +296,15 @@ struct Quantised {
     }
     // the code word of a unit
     static __device__ __forceinline__ uint32_t unit(const float (&x)[8], float zero, const Divisor& by) {
+        const Two z(zero, zero), up(ROUND, ROUND);
         float c[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)                               // (a NaN gets code 0)
-            c[i] = __fadd_rn(__fadd_rn(fminf(fmaxf(by.quotient(x[i] - zero), 0.f), 15.f), ROUND), -ROUND);
+        for (int i = 0; i < 8; i += 2) {
+            float t0, t1;
+            by.quotient(Two(x[i], x[i + 1]) - z).get(t0, t1);
+            t0 = fminf(fmaxf(t0, 0.f), 15.f); t1 = fminf(fmaxf(t1, 0.f), 15.f);       // (a NaN gets code 0)
+            (up - (Two(t0, t1) + up)).get(c[i], c[i + 1]);
+        }
         return pack_codes(c);
     }
     // The same of a key, not to the last bit: t = (x - zero) r / 15 in [0, 1] by one multiply-add that saturates, and how far
@@ -253,13 +312,17 @@ struct Quantised {
     // 2^-24 (7 |zero| / s + 63), and what difference and quotient are off by where the code is defined, 2^-24 31.
     static __device__ __forceinline__ uint32_t unit_near(const float (&x)[8], const float (&d)[8], float zero, float r, float& worst) {
         const float r15 = r * (1.f / 15.f), z15 = -zero * r15, off = fmaf(fabsf(z15), 7e-6f, 7e-6f);
-        float c[8];
+        const Two fifteen(15.f, 15.f), up(ROUND, ROUND);
+        float c[8], far = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float t = __saturatef(fmaf(x[i], r15, z15));
-            c[i] = __fadd_rn(__fmaf_rn(t, 15.f, ROUND), -ROUND);
-            worst = fmaxf(worst, fmaf(d[i], r, fabsf(fmaf(t, 15.f, -c[i]))) + off);
+        for (int i = 0; i < 8; i += 2) {
+            const Two t(__saturatef(fmaf(x[i], r15, z15)), __saturatef(fmaf(x[i + 1], r15, z15))), minus = up - fma2(t, fifteen, up);
+            minus.get(c[i], c[i + 1]);
+            float e0, e1;
+            fma2(t, fifteen, minus).get(e0, e1);
+            far = fmaxf(far, fmaxf(fmaf(d[i], r, fabsf(e0)), fmaf(d[i + 1], r, fabsf(e1))));
         }
+        worst = fmaxf(worst, far + off);
         return pack_codes(c);
     }
     static __device__ __noinline__ uint32_t unit_divided(float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7, float zero, float scale) {
@@ -421,7 +484,7 @@ novakv_rotate_kernel(const __grid_constant__ RotateArgs a) {
             float x[8], y[8];
             unpack_unit(r.x, x);
             unpack_unit(r.y, y);
-            transform_row<D, IL>(a, turn, ka, kb, x, y);
+            transform_row<D, IL, DST == DST_INT4>(a, turn, ka, kb, x, y);
             if (h + sub < a.hq) {
                 store_unit<VEC>(out + h * D + 8 * ka, pack_unit(x));
                 store_unit<VEC>(out + h * D + 8 * kb, pack_unit(y));
@@ -441,7 +504,7 @@ novakv_rotate_kernel(const __grid_constant__ RotateArgs a) {
             float x[8], y[8];
             unpack_unit(r.x, x);
             unpack_unit(r.y, y);
-            bool sure = transform_row<D, IL>(a, turn, ka, kb, x, y);
+            bool sure = transform_row<D, IL, DST == DST_INT4>(a, turn, ka, kb, x, y);
             if constexpr (DST == DST_INT4) {
                 uint8_t* chunk = a.k_pages + ((size_t)page * a.hkv + h + sub) * I4Layout<D>::CHUNK_BYTES;
                 Quantised<D, true> code;
