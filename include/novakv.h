@@ -421,7 +421,8 @@ novakv_status novakv_int4_gather(novakv_ctx* ctx, const int32_t* tok_seq, const 
  * measured) of what one step of a key's code moves it by in the query's largest channel.
  *   q    bf16 [batch][Hq][d], 16-byte aligned
  *   out  [batch][Hq][d], float32 if out_is_fp32 (8-byte aligned) else bf16 (4-byte aligned)
- *   workspace  novakv_int4_workspace_bytes(ctx, batch) bytes, 256-byte aligned; contents are scratch
+ *   workspace  novakv_int4_workspace_bytes(ctx, batch) bytes, 256-byte aligned; contents are scratch, which calls that may overlap
+ *              (other streams, graphs replayed side by side) must not share
  * A bad page id is replaced by page 0 and a bad length clamped (status bits).  A wait that gives up (novakv_debug_set_wait_limit)
  * sets NOVAKV_DEV_WAIT_TIMEOUT and leaves the call's output unspecified.  novakv_debug_set_scan_ctas applies.
  */

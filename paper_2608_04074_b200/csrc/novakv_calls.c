@@ -266,7 +266,7 @@ static int is_dtype(PyObject* x, PyObject* a, PyObject* b) {
 /* what is asked of argument `arg`; n: rows of the call, table_rows, pool_pages of its page table and its first pool */
 static int check(const Operator* e, char kind, int arg, PyObject* x, sizes* z, long long n, long long table_rows, long long pool_pages) {
     const int op = e->entry;
-    if (method_int(x, s_get_device) != e->device) return refuse(op, arg, "has to be a tensor on the context's device");
+    if (method_int(x, s_get_device) != e->device || PyErr_Occurred()) return refuse(op, arg, "has to be a tensor on the context's device");
     if (kind != 'w' && sizes_of(x, z)) return -1;
     const long long* v = z->size;
     switch (kind) {

@@ -673,6 +673,59 @@ def test_in_front_of_the_index_cache(contexts):
     assert torch.equal(*outs) and torch.isfinite(outs[0]).all()
 
 
+@pytest.mark.parametrize("shape", [(32, 8, 128), (64, 8, 64)])
+@pytest.mark.parametrize("cache", ["int4", "bf16"])
+def test_pools_beyond_32_bits(contexts, cache, shape):
+    """Pages behind the first 4 GB of a pool: what a small pool of the same pages gives."""
+    hq, hkv, d = shape
+    ctx, gen, n = contexts(shape), np.random.default_rng(72), 200
+    tr, _, _ = make_transform(gen, d, False, d)
+    page = ctx.novakv_int4_page_bytes() if cache == "int4" else hkv * 64 * d * 2
+    pages = (9 << 29) // page                                 # 4.5 GB
+    assert pages * page > 1 << 32
+    order = np.array([pages - 1, 0, pages - 3, pages // 2], np.int32)
+    k, v, q = bf16(draw(gen, n, hkv, d)), bf16(draw(gen, n, hkv, d)), bf16(draw(gen, 1, hq, d) * 2)
+    seq, pos, outs = dev(np.zeros(n, np.int32)), dev(np.arange(n, dtype=np.int32)), []
+    for total, table in ((pages, order), (4, np.arange(4, dtype=np.int32))):
+        if cache == "int4":
+            pools = [torch.empty((total, page), dtype=torch.uint8, device="cuda") for _ in range(2)]
+            ws = torch.empty(ctx.novakv_int4_workspace_bytes(1), dtype=torch.uint8, device="cuda")
+        else:
+            pools = [torch.empty((total, hkv, 64, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+            ws = torch.empty(ctx.novakv_bf16_workspace_bytes(1, 4), dtype=torch.uint8, device="cuda")
+        table, lens, out = dev(table[None]), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros((1, hq, d), device="cuda")
+        if cache == "int4":
+            ctx.novakv_int4_append(tr, k, v, seq, pos, *pools, table, lens)
+            rows = [torch.zeros((n, hkv, d), device="cuda") for _ in range(2)]
+            ctx.novakv_int4_gather(seq, pos, *pools, table, *rows)
+            ctx.novakv_int4_decode_attention(q, *pools, table, lens, out, ws)
+        else:
+            ctx.novakv_bf16_append(tr, k, v, seq, pos, *pools, table, lens)
+            rows = [p[table[0].long()[pos.long() // 64], :, pos.long() % 64].float() for p in pools]
+            ctx.novakv_bf16_decode_attention(q, *pools, table, lens, out, ws)
+        assert ctx.novakv_last_device_status() == 0 and lens.item() == n
+        outs.append([*rows, out])
+        del pools
+    assert all(torch.equal(a, b) for a, b in zip(*outs)) and torch.isfinite(outs[0][2]).all()
+
+
+def test_first_call_inside_a_capture():
+    """A context's first calls, captured: nothing of their set-up may need a stream that is not capturing."""
+    from paper_2608_04074_b200.binding import Context
+    shape = (4, 2, 64)
+    ctx, c = Context(*shape), Cache4(shape, [100, 70], 73)
+    out = torch.zeros((2, 4, 64), device="cuda")
+    ws = torch.empty(ctx.novakv_int4_workspace_bytes(2), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.novakv_int4_decode_attention(*c.dev, out, ws)
+    graph.replay()
+    torch.cuda.synchronize()
+    c.check(out)
+    ctx.close()
+
+
 def test_two_streams_with_workspaces_of_their_own(contexts):
     shape = (32, 8, 128)
     ctx = contexts(shape)
