@@ -370,7 +370,8 @@ novakv_status novakv_qk_norm_rope(novakv_ctx* ctx, const novakv_qk_transform* tr
  * Append to the BF16 cache that novakv_bf16_decode_attention reads (pools bf16 [n_pages][Hkv][64][d], 16-byte aligned): the
  * keys go through `transform` (NULL: as they are) with position tok_pos[t], the values do not; both land in slot tok_pos[t] % 64
  * of page page_table[tok_seq[t]][tok_pos[t] / 64], and seq_lens[tok_seq[t]] becomes max(seq_lens[tok_seq[t]], tok_pos[t] + 1).
- * q, q_out: the tokens' queries through the same transform in the same pass; both NULL: none.
+ * q, q_out: the tokens' queries through the same transform in the same pass; both NULL: none.  (novakv_decode_attention and its
+ * variants must not be the library call directly behind this one if they read q_out; the BF16 and 4-bit decode calls may be.)
  * Token lists, unused entries (tok_seq[t] = -1), skipped tokens and status bits are those of novakv_encode_append; the q_out
  * row of an entry that is skipped is left as it was.  Two tokens of one call that name one slot leave either's bytes in it, or a
  * mixture.

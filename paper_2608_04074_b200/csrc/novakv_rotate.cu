@@ -74,10 +74,8 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-template <typename T>
-__device__ __forceinline__ uint4 pack_unit(const T (&x)[8]) {
-    return make_uint4(pack2((float)x[0], (float)x[1]), pack2((float)x[2], (float)x[3]), pack2((float)x[4], (float)x[5]),
-                      pack2((float)x[6], (float)x[7]));
+__device__ __forceinline__ uint4 pack_unit(const float (&x)[8]) {
+    return make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
 }
 // two binary32 numbers side by side: one instruction does both (the append is bound by their number)
 struct Two {
