@@ -19,8 +19,8 @@
 //  * Join: what a warp has of a (sequence, KV head) pair that it does not hold whole goes to shared memory; the CTA joins these
 //    pieces, and a second kernel joins the at most two per CTA that reach over its ends.
 //
-// B200, bf16 output, 6.56 TB/s of measured copy bandwidth: 64 x 16384 tokens (32 / 8 heads, d = 128) 190 us, 97 % of it; 8 x 16384 36.5 us,
-// 63 %, of which launches, the look-up of the first units and the join are 8.5; 16 x 65536 (64 / 8 heads, d = 64) 106 us, 87 %, and 125 where
+// B200, bf16 output, 6.56 TB/s of measured copy bandwidth: 64 x 16384 tokens (32 / 8 heads, d = 128) 189 us, 97 % of it; 8 x 16384 35 us,
+// 66 %, of which launches, the look-up of the first units and the join are 8; 16 x 65536 (64 / 8 heads, d = 64) 107 us, 86 %, and 125 where
 // it runs for seconds and the board's power limit takes the clock from 1.96 to 1.69 GHz: what is left is instructions (540 a unit).
 #include <math_constants.h>
 
@@ -208,7 +208,7 @@ __device__ __forceinline__ void unpack_bytes(uint32_t x, uint32_t (&c)[4]) {
 }
 
 // FINE: for binary32 outputs.  The products keep the bits that they would lose (unpack_codes) and the weights meet the codes as
-// binary16 pairs hi + lo, in two products (8 x 16384 tokens: 49 us against 36.5).  Without, each product of a logit is cut off at 2^-15 of
+// binary16 pairs hi + lo, in two products (8 x 16384 tokens: 47.6 us against 35).  Without, each product of a logit is cut off at 2^-15 of
 // what one step of its key's code moves it by in the query's largest channel (136 cuts at most, some 2^-11 in all as measured),
 // and a weight is off by 2^-12 of itself, at random: an eighth of the rounding of a bfloat16 output.
 template <int D, int HG, bool FINE>
@@ -221,7 +221,6 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
     // heads columns 4..7 repeat columns 0..3, and the lanes that hold them take the other token: one token for two heads each.
     constexpr bool SPLIT = HG < 8;
     constexpr int R = SPLIT ? 1 : 2, COLS = SPLIT ? 4 : 8;
-    constexpr bool BYTES = !FINE && D == 64;                      // (at d = 128 the registers for it are not there: 36.5 -> 37.1 us)
     extern __shared__ __align__(128) unsigned char smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, j = lane & 3, up = SPLIT ? j >> 1 : 0, jj = SPLIT ? j & 1 : j;
     int *prefix = reinterpret_cast<int*>(smem + P::PREFIX), *lens = reinterpret_cast<int*>(smem + P::LENS);
@@ -572,71 +571,68 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
             constexpr int SB = FINE ? 2 : 1;
 #pragma unroll
             for (int sb = 0; sb < S; sb += SB) {
-                uint32_t b_hi[SB][G][2], b_lo[SB][G][2];
-                float mid[G][4];
+                float p0[SB][R], p1[SB][R];
 #pragma unroll
-                for (int e = 0; e < SB; ++e) {
-                    const int s = sb + e;
+                for (int e = 0; e < SB; ++e)
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        const float p0 = ex2f(z0[s][r] - m0), p1 = ex2f(z1[s][r] - m1);
-                        l0 += p0; l1 += p1;
+                        p0[e][r] = ex2f(z0[sb + e][r] - m0); p1[e][r] = ex2f(z1[sb + e][r] - m1);
+                        l0 += p0[e][r]; l1 += p1[e][r];
+                    }
 #pragma unroll
-                        for (int g = 0; g < G; ++g) {
+                for (int g = 0; g < G; ++g) {                     // (a group's weights, then its two pieces: few registers at a time)
+                    uint32_t b_hi[SB][2], b_lo[SB][2];
+#pragma unroll
+                    for (int e = 0; e < SB; ++e)
+#pragma unroll
+                        for (int r = 0; r < R; ++r) {
+                            const int s = sb + e;
                             const float zero = FINE ? fmaf(8.f, vs[s][r][g], vz[s][r][g]) : vz[s][r][g];
-                            zs0[g] = fmaf(p0, zero, zs0[g]);
-                            zs1[g] = fmaf(p1, zero, zs1[g]);
-                            const float f = vfac * vs[s][r][g], w0 = p0 * f, w1 = p1 * f;
+                            zs0[g] = fmaf(p0[e][r], zero, zs0[g]);
+                            zs1[g] = fmaf(p1[e][r], zero, zs1[g]);
+                            const float f = vfac * vs[s][r][g], w0 = p0[e][r] * f, w1 = p1[e][r] * f;
                             const uint32_t hi16 = pack_half(w0, w1), x = movmatrix_t(hi16);
                             // SPLIT: columns 0..3 take the lower eight tokens, columns 4..7 the upper ones
-                            if (SPLIT) { b_hi[e][g][0] = gr < 4 ? x : 0u; b_hi[e][g][1] = gr < 4 ? 0u : x; }
-                            else b_hi[e][g][r] = x;
+                            if (SPLIT) { b_hi[e][0] = gr < 4 ? x : 0u; b_hi[e][1] = gr < 4 ? 0u : x; }
+                            else b_hi[e][r] = x;
                             if (FINE) {
                                 const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi16));
                                 const uint32_t y = movmatrix_t(pack_half(w0 - back.x, w1 - back.y));
-                                if (SPLIT) { b_lo[e][g][0] = gr < 4 ? y : 0u; b_lo[e][g][1] = gr < 4 ? 0u : y; }
-                                else b_lo[e][g][r] = y;
+                                if (SPLIT) { b_lo[e][0] = gr < 4 ? y : 0u; b_lo[e][1] = gr < 4 ? 0u : y; }
+                                else b_lo[e][r] = y;
                             }
                         }
-                    }
-                }
-                if (FINE) {
-                    constexpr uint32_t M8 = 0x82008200u;          // -8 2^-18 twice
-#pragma unroll
-                    for (int g = 0; g < G; ++g) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) mid[g][i] = 0.f;
+                    float mid[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (FINE) {
+                        constexpr uint32_t M8 = 0x82008200u;      // -8 2^-18 twice
 #pragma unroll
                         for (int e = 0; e < SB; ++e) {
-                            mma16816(mid[g], M8, M8, M8, M8, b_hi[e][g][0], b_hi[e][g][1]);
-                            mma16816(mid[g], M8, M8, M8, M8, b_lo[e][g][0], b_lo[e][g][1]);
+                            mma16816(mid, M8, M8, M8, M8, b_hi[e][0], b_hi[e][1]);
+                            mma16816(mid, M8, M8, M8, M8, b_lo[e][0], b_lo[e][1]);
                         }
                     }
-                }
-#pragma unroll
-                for (int pp = 0; pp < NP; pp += 2) {
                     uint32_t r[SB][4];
 #pragma unroll
-                    for (int e = 0; e < SB; ++e) ldmatrix4t((vbase + mat ^ pp << 4) + (sb + e) / 2 * TB + (sb + e) % 2 * 16 * Lay::ROW, r[e]);
+                    for (int e = 0; e < SB; ++e) ldmatrix4t((vbase + mat ^ 2 * g << 4) + (sb + e) / 2 * TB + (sb + e) % 2 * 16 * Lay::ROW, r[e]);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const int p = pp + h, g = p / 2;
+                        const int p = 2 * g + h;
                         uint32_t x[SB][4], y[SB][4];
 #pragma unroll
                         for (int e = 0; e < SB; ++e) {
-                            if (BYTES) { unpack_bytes(r[e][2 * h], x[e]); unpack_bytes(r[e][2 * h + 1], y[e]); }
+                            if (!FINE) { unpack_bytes(r[e][2 * h], x[e]); unpack_bytes(r[e][2 * h + 1], y[e]); }
                             else { unpack_codes<FINE>(r[e][2 * h], x[e]); unpack_codes<FINE>(r[e][2 * h + 1], y[e]); }
                         }
 #pragma unroll
                         for (int sh = 0; sh < 2; ++sh) {
                             if (!FINE) {
-                                mma16816(o[p][sh], x[0][2 * sh], x[0][2 * sh + 1], y[0][2 * sh], y[0][2 * sh + 1], b_hi[0][g][0], b_hi[0][g][1]);
+                                mma16816(o[p][sh], x[0][2 * sh], x[0][2 * sh + 1], y[0][2 * sh], y[0][2 * sh + 1], b_hi[0][0], b_hi[0][1]);
                             } else {
-                                float sum[4] = {mid[g][0], mid[g][1], mid[g][2], mid[g][3]};
+                                float sum[4] = {mid[0], mid[1], mid[2], mid[3]};
 #pragma unroll
                                 for (int e = 0; e < SB; ++e) {
-                                    mma16816(sum, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_hi[e][g][0], b_hi[e][g][1]);
-                                    mma16816(sum, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_lo[e][g][0], b_lo[e][g][1]);
+                                    mma16816(sum, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_hi[e][0], b_hi[e][1]);
+                                    mma16816(sum, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_lo[e][0], b_lo[e][1]);
                                 }
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) o[p][sh][i] += sum[i];
@@ -682,7 +678,7 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
                 float v[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    v[i] = i < 2 && BYTES ? o[p][s][i] - o[p][s][i + 2] : o[p][s][i];
+                    v[i] = i < 2 && !FINE ? o[p][s][i] - o[p][s][i + 2] : o[p][s][i];
                     if (SPLIT) v[i] += __shfl_xor_sync(0xffffffffu, v[i], 2);
                     v[i] = fmaf(v[i] * (i < 2 || FINE ? UNIT : UNIT * 0.0625f), vbound, (i & 1) ? zs1[p / 2] : zs0[p / 2]);
                 }
