@@ -21,7 +21,7 @@
 //
 // B200, bf16 output, 6.56 TB/s of measured copy bandwidth: 64 x 16384 tokens (32 / 8 heads, d = 128) 189 us, 97 % of it; 8 x 16384 35 us,
 // 66 %, of which launches, the look-up of the first units and the join are 8; 16 x 65536 (64 / 8 heads, d = 64) 107 us, 86 %, and 125 where
-// it runs for seconds and the board's power limit takes the clock from 1.96 to 1.69 GHz: what is left is instructions (540 a unit).
+// it runs for seconds and the board's power limit takes the clock from 1.96 to 1.69 GHz: what is left is instructions (530 a unit).
 #include <math_constants.h>
 
 #include "novakv_int4.cuh"
