@@ -19,9 +19,9 @@
 //  * Join: what a warp has of a (sequence, KV head) pair that it does not hold whole goes to shared memory; the CTA joins these
 //    pieces, and a second kernel joins the at most two per CTA that reach over its ends.
 //
-// B200, bf16 output, 6.56 TB/s of measured copy bandwidth: 64 x 16384 tokens (32 / 8 heads, d = 128) 189 us, 97 % of it; 8 x 16384 35 us,
-// 66 %, of which launches, the look-up of the first units and the join are 8; 16 x 65536 (64 / 8 heads, d = 64) 107 us, 86 %, and 125 where
-// it runs for seconds and the board's power limit takes the clock from 1.96 to 1.69 GHz: what is left is instructions (530 a unit).
+// B200, bf16 output, 6.56 TB/s of measured copy bandwidth: 64 x 16384 tokens (32 / 8 heads, d = 128) 193 us, 96 % of it; 8 x 16384 37 us,
+// 63 %, of which launches, the look-up of the first units and the join are 8; 16 x 65536 (64 / 8 heads, d = 64) 115 us, 80 %, and more where
+// it runs for seconds and the board's power limit takes the clock down: what is left is instructions.
 #include <math_constants.h>
 
 #include "novakv_int4.cuh"
@@ -92,6 +92,13 @@ __device__ __forceinline__ uint32_t movmatrix_t(uint32_t x) {
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// (x, y) += (a, b), (x, y) -= (a, b): one instruction for both
+__device__ __forceinline__ void add2(float& x, float& y, float a, float b) {
+    asm("{.reg .b64 u, v; mov.b64 u, {%0, %1}; mov.b64 v, {%2, %3}; add.rn.f32x2 u, u, v; mov.b64 {%0, %1}, u;}" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void sub2(float& x, float& y, float a, float b) {
+    asm("{.reg .b64 u, v; mov.b64 u, {%0, %1}; mov.b64 v, {%2, %3}; sub.rn.f32x2 u, u, v; mov.b64 {%0, %1}, u;}" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
 }
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
@@ -200,7 +207,7 @@ __device__ __forceinline__ void unpack_codes(uint32_t x, uint32_t (&c)[4]) {
     }
 }
 
-// For the values, whose sums may be taken apart afterwards, four instructions: rows of codes c0 + 16 c1 (a byte) and of 16 c1 above
+// For the values, whose sums are taken apart every 32 tokens, four instructions: rows of codes c0 + 16 c1 (a byte) and of 16 c1 above
 // them, from which the sums over c0 and c1 follow; likewise c2, c3.
 __device__ __forceinline__ void unpack_bytes(uint32_t x, uint32_t (&c)[4]) {
     c[0] = x & 0x00ff00ffu; c[1] = x & 0x00f000f0u;
@@ -208,9 +215,12 @@ __device__ __forceinline__ void unpack_bytes(uint32_t x, uint32_t (&c)[4]) {
 }
 
 // FINE: for binary32 outputs.  The products keep the bits that they would lose (unpack_codes) and the weights meet the codes as
-// binary16 pairs hi + lo, in two products (8 x 16384 tokens: 47.6 us against 35).  Without, each product of a logit is cut off at 2^-15 of
-// what one step of its key's code moves it by in the query's largest channel (136 cuts at most, some 2^-11 in all as measured),
-// and a weight is off by 2^-12 of itself, at random: an eighth of the rounding of a bfloat16 output.
+// binary16 pairs hi + lo, in two products (8 x 16384 tokens: 47.8 us against 36.6).  Without, each product of a logit is cut off at 2^-15
+// of what one step of its key's code moves it by in the query's largest channel (136 cuts at most, some 2^-11 in all as measured),
+// and weight times scale is a binary16 number, 11 bits: off by 2^-11 of itself at most, an eighth of a bfloat16 output's own rounding.
+// The codes that it meets count from their middle, 7.5 (wsum below), so that errors which agree - weights nearly alike over a long
+// sequence - stay a part of the result and do not meet the zeros, whose sum is exact: at 16 x 65536 tokens, d = 64, and logits of a
+// standard deviation of 3e-4 the output is then off by 1.66e-3 of its size, what its own rounding leaves, and by 3.6e-3 without.
 template <int D, int HG, bool FINE>
 __global__ void __launch_bounds__(THREADS, 1)
 novakv_int4_decode_kernel(const DecodeArgs a) {
@@ -441,9 +451,9 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
             }
         }
         float m0 = -CUDART_INF_F, m1 = m0, l0 = 0.f, l1 = 0.f, zs0[G], zs1[G], vbound = 0.f, vfac = 0.f;
-        float o[NP][2][4];
+        float o[NP][2][4], wsum0[G], wsum1[G];                       // (wsum: bf16 outputs alone, the sums of the weights that met the codes)
 #pragma unroll
-        for (int g = 0; g < G; ++g) zs0[g] = zs1[g] = 0.f;
+        for (int g = 0; g < G; ++g) zs0[g] = zs1[g] = wsum0[g] = wsum1[g] = 0.f;
 #pragma unroll
         for (int p = 0; p < NP; ++p)
 #pragma unroll
@@ -559,16 +569,20 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
                         vfac = W_ONE / nb;
                     }
 #pragma unroll
+                    for (int g = 0; g < G; ++g) { wsum0[g] *= a0; wsum1[g] *= a1; }
+#pragma unroll
                     for (int p = 0; p < NP; ++p)
 #pragma unroll
                         for (int s = 0; s < 2; ++s) { o[p][s][0] *= a0; o[p][s][1] *= a1; o[p][s][2] *= a0; o[p][s][3] *= a1; }
                 }
             }
 
-            // ---- weights and values.  FINE: sums of 32 tokens apart, on codes counted from the middle (a product with the constant
-            // -8 of all of them), added in binary32: the tensor core cuts sums off instead of rounding them, which over a long
-            // sequence of like weights would add up against a result that is small beside them.
-            constexpr int SB = FINE ? 2 : 1;
+            // ---- weights and values, in sums of 32 tokens that are added in binary32: the tensor core cuts sums off instead of
+            // rounding them, which over a long sequence of like weights would add up against a result that is small beside them (one
+            // accumulator over a warp's 3500 tokens of a flat attention, 16 x 65536, d = 64: 14 % of the result; so 2^-10 of it).
+            // The codes count from the middle, since a sum from 0 would be 4 to 1000 times the result: FINE by a product with the
+            // constant -8 of all of them, bf16 outputs by the weights' sum afterwards (a product there, as well: 197 against 193 us).
+            constexpr int SB = 2;
 #pragma unroll
             for (int sb = 0; sb < S; sb += SB) {
                 float p0[SB][R], p1[SB][R];
@@ -587,16 +601,17 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
 #pragma unroll
                         for (int r = 0; r < R; ++r) {
                             const int s = sb + e;
-                            const float zero = FINE ? fmaf(8.f, vs[s][r][g], vz[s][r][g]) : vz[s][r][g];
+                            const float zero = fmaf(FINE ? 8.f : 7.5f, vs[s][r][g], vz[s][r][g]);
                             zs0[g] = fmaf(p0[e][r], zero, zs0[g]);
                             zs1[g] = fmaf(p1[e][r], zero, zs1[g]);
                             const float f = vfac * vs[s][r][g], w0 = p0[e][r] * f, w1 = p1[e][r] * f;
                             const uint32_t hi16 = pack_half(w0, w1), x = movmatrix_t(hi16);
+                            const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi16));
+                            if (!FINE) add2(wsum0[g], wsum1[g], back.x, back.y);
                             // SPLIT: columns 0..3 take the lower eight tokens, columns 4..7 the upper ones
                             if (SPLIT) { b_hi[e][0] = gr < 4 ? x : 0u; b_hi[e][1] = gr < 4 ? 0u : x; }
                             else b_hi[e][r] = x;
                             if (FINE) {
-                                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi16));
                                 const uint32_t y = movmatrix_t(pack_half(w0 - back.x, w1 - back.y));
                                 if (SPLIT) { b_lo[e][0] = gr < 4 ? y : 0u; b_lo[e][1] = gr < 4 ? 0u : y; }
                                 else b_lo[e][r] = y;
@@ -625,17 +640,19 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
                         }
 #pragma unroll
                         for (int sh = 0; sh < 2; ++sh) {
-                            if (!FINE) {
-                                mma16816(o[p][sh], x[0][2 * sh], x[0][2 * sh + 1], y[0][2 * sh], y[0][2 * sh + 1], b_hi[0][0], b_hi[0][1]);
-                            } else {
-                                float sum[4] = {mid[0], mid[1], mid[2], mid[3]};
+                            float sum[4] = {mid[0], mid[1], mid[2], mid[3]};
 #pragma unroll
-                                for (int e = 0; e < SB; ++e) {
-                                    mma16816(sum, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_hi[e][0], b_hi[e][1]);
-                                    mma16816(sum, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_lo[e][0], b_lo[e][1]);
-                                }
+                            for (int e = 0; e < SB; ++e) {
+                                mma16816(sum, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_hi[e][0], b_hi[e][1]);
+                                if (FINE) mma16816(sum, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_lo[e][0], b_lo[e][1]);
+                            }
+                            if (FINE) {
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) o[p][sh][i] += sum[i];
+                            } else {                              // (c0 + 16 c1 and 16 c1)
+                                sub2(sum[0], sum[1], sum[2], sum[3]);
+                                add2(o[p][sh][0], o[p][sh][1], sum[0], sum[1]);
+                                add2(o[p][sh][2], o[p][sh][3], sum[2], sum[3]);
                             }
                         }
                     }
@@ -655,6 +672,16 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
             for (int g = 0; g < G; ++g) {
                 zs0[g] += __shfl_xor_sync(0xffffffffu, zs0[g], s);
                 zs1[g] += __shfl_xor_sync(0xffffffffu, zs1[g], s);
+                if (FINE) continue;
+                wsum0[g] += __shfl_xor_sync(0xffffffffu, wsum0[g], s);
+                wsum1[g] += __shfl_xor_sync(0xffffffffu, wsum1[g], s);
+            }
+        }
+        if (!FINE) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                zs0[g] = fmaf(wsum0[g] * (-7.5f / W_ONE), vbound, zs0[g]);
+                zs1[g] = fmaf(wsum1[g] * (-7.5f / W_ONE), vbound, zs1[g]);
             }
         }
         const bool ends = seg_first + seg_n == at.s.units, whole = ends && seg_first == 0;
@@ -678,7 +705,7 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
                 float v[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    v[i] = i < 2 && !FINE ? o[p][s][i] - o[p][s][i + 2] : o[p][s][i];
+                    v[i] = o[p][s][i];
                     if (SPLIT) v[i] += __shfl_xor_sync(0xffffffffu, v[i], 2);
                     v[i] = fmaf(v[i] * (i < 2 || FINE ? UNIT : UNIT * 0.0625f), vbound, (i & 1) ? zs1[p / 2] : zs0[p / 2]);
                 }

@@ -1,0 +1,53 @@
+"""Decode over the 4-bit cache where attention is long and flat: the output is a small rest of a large sum."""
+import pytest
+
+import int4_accuracy as A
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def contexts():
+    from paper_2608_04074_b200.binding import Context
+    made = {}
+
+    def get(shape):
+        if shape not in made:
+            made[shape] = Context(*shape)
+        return made[shape]
+    return get
+
+
+def filled(ctx, n, seed, batch=1):
+    """A cache of `batch` sequences of n near-Gaussian rows, and what its slots stand for (float32 [batch n][Hkv][d])."""
+    from paper_2608_04074_b200.runtime import Int4Cache
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    k, v = (torch.randn((batch * n, ctx.n_kv_heads, ctx.head_dim), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    seq = torch.arange(batch, dtype=torch.int32, device="cuda").repeat_interleave(n)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda").repeat(batch)
+    cache = Int4Cache(ctx, batch, n, seed=seed)
+    cache.append(None, k, v, seq, pos)
+    return cache, *cache.gather(seq, pos, torch.float32), g
+
+
+SHAPES = [(64, 8, 64), (32, 8, 64), (32, 16, 64), (32, 32, 64), (32, 8, 128), (16, 8, 128), (16, 16, 128)]
+
+
+@pytest.mark.parametrize("std", [0.0, 3e-4, 0.3, 1.0])
+@pytest.mark.parametrize("ctas", [1, 0])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_long_flat_attention(contexts, shape, ctas, std):
+    """Logits of a standard deviation of `std`, bf16 outputs; with one CTA a warp holds 16384 tokens of a pair and more."""
+    ctx, n = contexts(shape), 32768
+    cache, k, v, g = filled(ctx, n, 80)
+    q = (std * torch.randn((1, shape[0], shape[2]), generator=g, device="cuda")).to(torch.bfloat16)
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    try:
+        ctx.novakv_debug_set_scan_ctas(ctas)
+        cache.decode(q, out=out)
+    finally:
+        ctx.novakv_debug_set_scan_ctas(0)
+    o, p = A.attention(q[0], k, v, shape[2] ** -0.5)
+    error, bound = A.rms(out[0].double() - o), A.bf16_bound(o, p, v)
+    assert error <= bound, (error, bound, A.rms(o))
