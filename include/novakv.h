@@ -158,7 +158,8 @@ novakv_status novakv_encode_append(novakv_ctx* ctx, int layer,
  * on tensor cores, others from a binary32 table; against binary64 neither output is further off than the other by more than
  * the weights' rounding.
  * q is read as soon as the kernel before this call in `stream` lets its dependents start: it must not be the output of the
- * library call directly before this one.
+ * library call directly before this one, unless that is novakv_qk_norm_rope, novakv_bf16_append or novakv_int4_append, whose
+ * queries this call and its variants wait for.
  *   q    bf16 [batch][Hq][d]
  *   out  [batch][Hq][d], float32 if out_is_fp32 else bf16; a sequence of length 0 yields zeros
  *   workspace  at least novakv_decode_workspace_bytes(ctx, batch) bytes; contents are scratch
@@ -360,7 +361,6 @@ typedef struct {
  *            cut out of a fused projection); heads of a token are contiguous.  Either may be NULL together with its output.
  *   q_out, k_out  bf16, laid out the same way; an output may be its own input with the same stride, else they must not overlap
  *   tok_pos  int32 [n_tokens], any value.  Rows 16-byte aligned (pointer and stride) are faster, others are taken.
- * (novakv_decode_attention must not be the library call directly behind this one if it reads its q: see there.)
  */
 novakv_status novakv_qk_norm_rope(novakv_ctx* ctx, const novakv_qk_transform* transform, const void* q, long long q_stride,
     const void* k, long long k_stride, const int32_t* tok_pos, int n_tokens, void* q_out, long long q_out_stride,
@@ -370,8 +370,7 @@ novakv_status novakv_qk_norm_rope(novakv_ctx* ctx, const novakv_qk_transform* tr
  * Append to the BF16 cache that novakv_bf16_decode_attention reads (pools bf16 [n_pages][Hkv][64][d], 16-byte aligned): the
  * keys go through `transform` (NULL: as they are) with position tok_pos[t], the values do not; both land in slot tok_pos[t] % 64
  * of page page_table[tok_seq[t]][tok_pos[t] / 64], and seq_lens[tok_seq[t]] becomes max(seq_lens[tok_seq[t]], tok_pos[t] + 1).
- * q, q_out: the tokens' queries through the same transform in the same pass; both NULL: none.  (novakv_decode_attention and its
- * variants must not be the library call directly behind this one if they read q_out; the BF16 and 4-bit decode calls may be.)
+ * q, q_out: the tokens' queries through the same transform in the same pass; both NULL: none.
  * Token lists, unused entries (tok_seq[t] = -1), skipped tokens and status bits are those of novakv_encode_append; the q_out
  * row of an entry that is skipped is left as it was.  Two tokens of one call that name one slot leave either's bytes in it, or a
  * mixture.

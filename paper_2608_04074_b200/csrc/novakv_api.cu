@@ -27,6 +27,70 @@ extern "C" const char* novakv_status_string(novakv_status s) {
     return "unknown status";
 }
 
+// ------------------------------------------------------------------ streams that end in a kernel that writes queries
+namespace {
+
+struct query_writer {
+    cudaStream_t stream;
+    int device;                             // of the default streams, whose handles every device and thread shares
+    const void* thread;
+    unsigned long long capture;             // 0: not captured
+    bool operator==(const query_writer& o) const {
+        return stream == o.stream && device == o.device && thread == o.thread && capture == o.capture;
+    }
+};
+constexpr int MAX_QUERY_WRITERS = 64;       // more of them at once: from then on no query transform overlaps the kernel in front
+query_writer g_writers[MAX_QUERY_WRITERS];
+std::atomic_flag g_writers_lock = ATOMIC_FLAG_INIT;
+thread_local char t_self;
+
+query_writer writer_of(cudaStream_t stream) {
+    query_writer w = {stream == cudaStreamLegacy ? nullptr : stream, 0, stream == cudaStreamPerThread ? &t_self : nullptr, 0};
+    if (w.stream == nullptr || w.stream == cudaStreamPerThread) cudaGetDevice(&w.device);
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    if (w.stream != nullptr && cudaStreamGetCaptureInfo(stream, &status, &w.capture) != cudaSuccess) cudaGetLastError();
+    if (status != cudaStreamCaptureStatusActive) w.capture = 0;       // (the default stream cannot be captured)
+    return w;
+}
+struct writers_guard {
+    writers_guard() { while (g_writers_lock.test_and_set(std::memory_order_acquire)) {} }
+    ~writers_guard() { g_writers_lock.clear(std::memory_order_release); }
+};
+
+}  // namespace
+
+std::atomic<int> novakv_query_writers{0};
+
+void novakv_queries_written(cudaStream_t stream) {
+    const query_writer w = writer_of(stream);
+    const writers_guard guard;
+    const int n = novakv_query_writers.load(std::memory_order_relaxed);
+    for (int i = 0; i < n && i < MAX_QUERY_WRITERS; ++i)
+        if (g_writers[i] == w) return;
+    if (n < MAX_QUERY_WRITERS) g_writers[n] = w;
+    if (n <= MAX_QUERY_WRITERS) novakv_query_writers.store(n + 1, std::memory_order_relaxed);
+}
+void novakv_queries_settled(cudaStream_t stream) {
+    const query_writer w = writer_of(stream);
+    const writers_guard guard;
+    const int n = novakv_query_writers.load(std::memory_order_relaxed);
+    for (int i = 0; i < n && n <= MAX_QUERY_WRITERS; ++i)
+        if (g_writers[i] == w) {
+            g_writers[i] = g_writers[n - 1];
+            novakv_query_writers.store(n - 1, std::memory_order_relaxed);
+            return;
+        }
+}
+bool novakv_queries_pending(cudaStream_t stream) {
+    if (novakv_query_writers.load(std::memory_order_relaxed) == 0) return false;
+    const query_writer w = writer_of(stream);
+    const writers_guard guard;
+    const int n = novakv_query_writers.load(std::memory_order_relaxed);
+    for (int i = 0; i < n && n <= MAX_QUERY_WRITERS; ++i)
+        if (g_writers[i] == w) return true;
+    return n > MAX_QUERY_WRITERS;
+}
+
 static bool shape_supported(const novakv_config& c) {
     if (c.group_size != NOVAKV_G || c.codebook_size != NOVAKV_C || c.page_tokens != NOVAKV_PAGE_TOKENS) return false;
     if (c.head_dim != 64 && c.head_dim != 128) return false;

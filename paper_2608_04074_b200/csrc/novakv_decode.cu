@@ -2334,7 +2334,8 @@ novakv_status launch_decode_t(novakv_ctx* ctx, const novakv_layer& ly, const __n
     // sequences per prepare block: one while all pairs fit on the machine twice over, then enough to make that so
     const int seqs_per_block = max(1, min(PREPARE_RUN, (batch * hkv + 2 * ctx->n_sm - 1) / (2 * ctx->n_sm)));
     auto prepare = seqs_per_block > 1 ? novakv_prepare_kernel<D, HG, true> : novakv_prepare_kernel<D, HG, false>;
-    novakv_launch_pdl(prepare, dim3((batch + seqs_per_block - 1) / seqs_per_block * hkv + (scan_prefix ? 0 : 1)), dim3(512), 0, stream, q, ly.rk_inv_t, seq_lens,
+    // (the query transform reads q before it waits: not while a kernel of the library still writes it)
+    novakv_launch(!novakv_queries_pending(stream), prepare, dim3((batch + seqs_per_block - 1) / seqs_per_block * hkv + (scan_prefix ? 0 : 1)), dim3(512), 0, stream, q, ly.rk_inv_t, seq_lens,
                       batch, hq, hkv, max_pages_per_seq, sm_scale * 1.4426950408889634f, qp, prefix, ctx->dev_status,
                       k_off_vec, qk_off, cost_prefix, ctx->seg_weight, (const float*)ly.k_center, qc,
                       fuse ? pair_count : (int32_t*)nullptr, fuse ? out : (void*)nullptr, out_is_fp32, seqs_per_block, scan_prefix ? 0 : 1);

@@ -684,11 +684,12 @@ novakv_status novakv_launch_encode(novakv_ctx* ctx, const novakv_layer& ly, cons
     int max_pages_per_seq, int n_seq, int32_t* seq_lens, cudaStream_t stream, __nv_bfloat16* k_scales,
     __nv_bfloat16* v_meta) {
     if (v_meta != nullptr && k_scales == nullptr) return NOVAKV_EUNSUPPORTED;   // INT2 values come with scaled keys
-    if (ctx->cfg.head_dim == 128)
-        return launch_encode_t<128>(ctx, ly, k_new, v_new, tok_seq, tok_pos, n_tokens, k_pages, v_pages, n_pages,
+    auto launch = ctx->cfg.head_dim == 128 ? launch_encode_t<128> : launch_encode_t<64>;
+    const novakv_status st = launch(ctx, ly, k_new, v_new, tok_seq, tok_pos, n_tokens, k_pages, v_pages, n_pages,
                                     page_table, max_pages_per_seq, n_seq, seq_lens, stream, k_scales, v_meta);
-    return launch_encode_t<64>(ctx, ly, k_new, v_new, tok_seq, tok_pos, n_tokens, k_pages, v_pages, n_pages,
-                               page_table, max_pages_per_seq, n_seq, seq_lens, stream, k_scales, v_meta);
+    // (for the launches that are not made by novakv_launch)
+    if (st == NOVAKV_OK && novakv_query_writers.load(std::memory_order_relaxed) != 0) novakv_queries_settled(stream);
+    return st;
 }
 
 // Gather of up to 5 page-locked host buffers into device staging: every word crosses the bus once, consecutive threads take

@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <stdint.h>
+#include <atomic>
 #include <vector>
 
 #include "novakv.h"
@@ -145,16 +146,26 @@ novakv_status novakv_launch_bf16_decode(novakv_ctx* ctx, const __nv_bfloat16* q,
 // and its writes are visible.  Before the wait a kernel only reads calibration constants (uploaded
 // synchronously by novakv_load_calibration, never written by a kernel) into registers or its own shared
 // memory, so the launch latency and that staging overlap the predecessor's tail; the query transform also reads q, which
-// the public header asks to be complete by then.  Nothing is written to global memory before the wait: workspaces, staging
+// the public header asks to be complete by then, and which is launched without the overlap directly behind a kernel
+// of the library that writes queries (below).  Nothing is written to global memory before the wait: workspaces, staging
 // buffers and freed tensors share memory with what the predecessor may still read.  There is no unbounded wait in user code.
 __device__ __forceinline__ void novakv_grid_dependency_wait() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// Streams whose last kernel of the library writes queries: what is launched behind it must not read them before it has
+// completed.  Any kernel of the library that waits for its predecessor in every block settles that, as does one that is
+// launched without the overlap.  The record is the process's own (another context may make the next call), and one of a
+// captured launch belongs to its capture.
+extern std::atomic<int> novakv_query_writers;                // entries of the record
+void novakv_queries_written(cudaStream_t stream);
+void novakv_queries_settled(cudaStream_t stream);
+bool novakv_queries_pending(cudaStream_t stream);
+
 template <typename... KArgs, typename... Args>
-cudaError_t novakv_launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream,
-                              Args... args) {
+cudaError_t novakv_launch(bool overlap, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream,
+                          Args... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
@@ -164,8 +175,15 @@ cudaError_t novakv_launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+    cfg.numAttrs = overlap ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+    if (e == cudaSuccess && novakv_query_writers.load(std::memory_order_relaxed) != 0) novakv_queries_settled(stream);
+    return e;
+}
+template <typename... KArgs, typename... Args>
+cudaError_t novakv_launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream,
+                              Args... args) {
+    return novakv_launch(true, kernel, grid, block, smem, stream, args...);
 }
 
 // Byte offsets inside the 64*L-byte chunk of one (page, KV head); t = token slot in the page

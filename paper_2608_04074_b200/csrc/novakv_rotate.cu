@@ -642,6 +642,7 @@ novakv_status launch_rotate_t(novakv_ctx* ctx, RotateArgs& a, bool vec, cudaStre
     const long long blocks = ((long long)a.n_tokens * a.parts + WARPS - 1) / WARPS;
     auto* kern = vec ? novakv_rotate_kernel<D, DST, true, IL> : novakv_rotate_kernel<D, DST, false, IL>;
     if (novakv_launch_pdl(kern, dim3((unsigned)blocks), dim3(ROT_THREADS), 0, stream, a) != cudaSuccess) return NOVAKV_ECUDA;
+    if (DST == DST_ROWS || a.hq > 0) novakv_queries_written(stream);       // (rows of either role: with as many heads they are alike)
     ctx->launches++;
     return NOVAKV_OK;
 }
