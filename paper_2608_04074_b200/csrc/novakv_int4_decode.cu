@@ -215,7 +215,7 @@ __device__ __forceinline__ void unpack_bytes(uint32_t x, uint32_t (&c)[4]) {
 }
 
 // FINE: for binary32 outputs.  The products keep the bits that they would lose (unpack_codes) and the weights meet the codes as
-// binary16 pairs hi + lo, in two products (8 x 16384 tokens: 47.8 us against 36.6).  Without, each product of a logit is cut off at 2^-15
+// binary16 pairs hi + lo, in two products (8 x 16384 tokens: 46.9 us against 36.8).  Without, each product of a logit is cut off at 2^-15
 // of what one step of its key's code moves it by in the query's largest channel (136 cuts at most, some 2^-11 in all as measured),
 // and weight times scale is a binary16 number, 11 bits: off by 2^-11 of itself at most, an eighth of a bfloat16 output's own rounding.
 // The codes that it meets count from their middle, 7.5 (wsum below), so that errors which agree - weights nearly alike over a long
@@ -580,8 +580,11 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
             // ---- weights and values, in sums of 32 tokens that are added in binary32: the tensor core cuts sums off instead of
             // rounding them, which over a long sequence of like weights would add up against a result that is small beside them (one
             // accumulator over a warp's 3500 tokens of a flat attention, 16 x 65536, d = 64: 14 % of the result; so 2^-10 of it).
-            // The codes count from the middle, since a sum from 0 would be 4 to 1000 times the result: FINE by a product with the
-            // constant -8 of all of them, bf16 outputs by the weights' sum afterwards (a product there, as well: 197 against 193 us).
+            // The codes count from their middle, 7.5, since a sum from 0 would be 4 to 1000 times the result: FINE by a product with the
+            // constant -7.5 of all of them, bf16 outputs by the weights' sum afterwards (a product there, as well: 197 against 193 us).
+            // FINE: hi and lo parts apart.  Sums over hi parts are exact (15 bits a product) while the weights of 32 tokens lie within
+            // 2^10 of one another; with lo parts in the same sum each of these was cut off at 2^-20 of a code's step, always towards
+            // zero: 4e-5 of a flat output over 32768 tokens, 2e-7 so, which is a binary32 evaluation's.
             constexpr int SB = 2;
 #pragma unroll
             for (int sb = 0; sb < S; sb += SB) {
@@ -601,7 +604,7 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
 #pragma unroll
                         for (int r = 0; r < R; ++r) {
                             const int s = sb + e;
-                            const float zero = fmaf(FINE ? 8.f : 7.5f, vs[s][r][g], vz[s][r][g]);
+                            const float zero = fmaf(7.5f, vs[s][r][g], vz[s][r][g]);
                             zs0[g] = fmaf(p0[e][r], zero, zs0[g]);
                             zs1[g] = fmaf(p1[e][r], zero, zs1[g]);
                             const float f = vfac * vs[s][r][g], w0 = p0[e][r] * f, w1 = p1[e][r] * f;
@@ -617,13 +620,13 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
                                 else b_lo[e][r] = y;
                             }
                         }
-                    float mid[4] = {0.f, 0.f, 0.f, 0.f};
+                    float mid[4] = {0.f, 0.f, 0.f, 0.f}, mid_lo[4] = {0.f, 0.f, 0.f, 0.f};
                     if (FINE) {
-                        constexpr uint32_t M8 = 0x82008200u;      // -8 2^-18 twice
+                        constexpr uint32_t M = 0x81e081e0u;       // -7.5 2^-18 twice
 #pragma unroll
                         for (int e = 0; e < SB; ++e) {
-                            mma16816(mid, M8, M8, M8, M8, b_hi[e][0], b_hi[e][1]);
-                            mma16816(mid, M8, M8, M8, M8, b_lo[e][0], b_lo[e][1]);
+                            mma16816(mid, M, M, M, M, b_hi[e][0], b_hi[e][1]);
+                            mma16816(mid_lo, M, M, M, M, b_lo[e][0], b_lo[e][1]);
                         }
                     }
                     uint32_t r[SB][4];
@@ -640,20 +643,20 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
                         }
 #pragma unroll
                         for (int sh = 0; sh < 2; ++sh) {
-                            float sum[4] = {mid[0], mid[1], mid[2], mid[3]};
+                            float sum[4] = {mid[0], mid[1], mid[2], mid[3]}, sum_lo[4] = {mid_lo[0], mid_lo[1], mid_lo[2], mid_lo[3]};
 #pragma unroll
                             for (int e = 0; e < SB; ++e) {
                                 mma16816(sum, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_hi[e][0], b_hi[e][1]);
-                                if (FINE) mma16816(sum, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_lo[e][0], b_lo[e][1]);
+                                if (FINE) mma16816(sum_lo, x[e][2 * sh], x[e][2 * sh + 1], y[e][2 * sh], y[e][2 * sh + 1], b_lo[e][0], b_lo[e][1]);
                             }
                             if (FINE) {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) o[p][sh][i] += sum[i];
+                                add2(sum[0], sum[1], sum_lo[0], sum_lo[1]);
+                                add2(sum[2], sum[3], sum_lo[2], sum_lo[3]);
                             } else {                              // (c0 + 16 c1 and 16 c1)
                                 sub2(sum[0], sum[1], sum[2], sum[3]);
-                                add2(o[p][sh][0], o[p][sh][1], sum[0], sum[1]);
-                                add2(o[p][sh][2], o[p][sh][3], sum[2], sum[3]);
                             }
+                            add2(o[p][sh][0], o[p][sh][1], sum[0], sum[1]);
+                            add2(o[p][sh][2], o[p][sh][3], sum[2], sum[3]);
                         }
                     }
                 }

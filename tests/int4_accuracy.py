@@ -30,3 +30,15 @@ def bf16_bound(o, p, v):
     half = (groups.amax(-1) - groups.amin(-1)) / 2                     # [n][Hkv][groups]
     weights = (2.0 ** -11 / 3 ** 0.5) ** 2 * torch.einsum("hgn,nhc->hgc", p.double() ** 2, half ** 2).mean().item()
     return 1.15 * (rms(o.to(torch.bfloat16).double() - o) ** 2 + weights) ** 0.5
+
+
+def float32_bound(o, o32, p, v):
+    """rms error of a float32 output.  o32: the same in torch's binary32, whose logits, exponentials and sums are rounded as often as
+    the kernel's (four times that for the order of the sums and the base-2 exponential).  Weights times scales are pairs of binary16
+    numbers, 22 bits, and the exponential is off by 2^-22: together 2^-21 of a weight, which meets half a group's range at most;
+    twice that.  A warp adds up n / 32 sums one after another at most (torch: in a tree), each sum rounded by 2^-25 of what there is
+    in the mean, at random; values and zeros apart, hence four times that."""
+    groups = v.double().unflatten(-1, (-1, 64))
+    half = (groups.amax(-1) - groups.amin(-1)) / 2
+    weights = 2.0 ** -20 * torch.einsum("hgn,nhc->hgc", p.double() ** 2, half ** 2).mean().sqrt().item()
+    return 4 * rms(o32.double() - o) + weights + 2.0 ** -23 * (len(v) / 32) ** 0.5 * rms(o)

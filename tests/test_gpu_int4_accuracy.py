@@ -51,3 +51,23 @@ def test_long_flat_attention(contexts, shape, ctas, std):
     o, p = A.attention(q[0], k, v, shape[2] ** -0.5)
     error, bound = A.rms(out[0].double() - o), A.bf16_bound(o, p, v)
     assert error <= bound, (error, bound, A.rms(o))
+
+
+@pytest.mark.parametrize("std", [0.0, 3e-4, 0.3, 1.0, 3.0, 8.0])
+@pytest.mark.parametrize("n,ctas", [(40, 0), (777, 0), (4097, 0), (32768, 0), (32768, 1)])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_float32_outputs(contexts, shape, n, ctas, std):
+    """What a float32 output is worth on ordinary data: that of a binary32 evaluation."""
+    ctx = contexts(shape)
+    cache, k, v, g = filled(ctx, n, 81)
+    q = (std * torch.randn((1, shape[0], shape[2]), generator=g, device="cuda")).to(torch.bfloat16)
+    sink = torch.randn(shape[0], generator=g, device="cuda")
+    try:
+        ctx.novakv_debug_set_scan_ctas(ctas)
+        out = cache.decode(q, sink_logits=sink)
+    finally:
+        ctx.novakv_debug_set_scan_ctas(0)
+    o, p = A.attention(q[0], k, v, shape[2] ** -0.5, sink=sink)
+    o32, _ = A.attention(q[0], k, v, shape[2] ** -0.5, torch.float32, sink=sink)
+    error, bound = A.rms(out[0].double() - o), A.float32_bound(o, o32, p, v)
+    assert error <= bound, (error, bound, A.rms(o))
