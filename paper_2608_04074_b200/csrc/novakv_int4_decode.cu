@@ -391,7 +391,7 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
     // lane's row of the matrix loads: token lane % 16 (of 16), piece lane / 16 (of two)
     const uint32_t mat = (lane & 15) * Lay::ROW + (((lane >> 4) ^ Lay::swizzle(lane & 15)) << 4);
     const uint32_t pairs = Lay::pair(8 * up + gr, 0);
-    bool given_up = false;
+    bool given_up = n > 0 && a.wait_clocks == 0;                  // (a limit of 0: before the first look)
     int t = 0;
 #pragma unroll 1
     while (t < n && !given_up) {
