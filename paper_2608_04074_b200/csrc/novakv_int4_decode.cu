@@ -417,7 +417,7 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
 #pragma unroll
             for (int s = 4; s < 32; s <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
             // 2^e brings the heads' largest coordinate just below 2^15 (what is 2^-31 of it or less loses bits)
-            const int e = min(max(15 - ((int)(__float_as_uint(mx) >> 23) - 126), -100), 120);
+            const int e = min(15 - ((int)(__float_as_uint(mx) >> 23) - 126), 120);
             const float f = __uint_as_float((uint32_t)(e + 127) << 23), odd = FINE ? f : f * 0.0625f;
             float sum[G];
 #pragma unroll
@@ -436,7 +436,8 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
                     qf[p][s][1] = pack_half(x[2 * s + 1] * odd, x[2 * s + 5] * odd);
                 }
             }
-            qfac = a.scale_log2 * __uint_as_float((uint32_t)((FINE ? 18 : 24) - e + 127) << 23);
+            const int back = (FINE ? 18 : 24) - e;                 // (-102 to 137: in two steps)
+            qfac = a.scale_log2 * __uint_as_float((uint32_t)(back / 2 + 127) << 23) * __uint_as_float((uint32_t)(back - back / 2 + 127) << 23);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 1);
