@@ -416,9 +416,11 @@ novakv_status novakv_int4_gather(novakv_ctx* ctx, const int32_t* tok_seq, const 
 /*
  * Decode attention over the 4-bit cache: for each sequence softmax(sm_scale q k^^T) v^ over positions 0 .. seq_lens[b] - 1, or its
  * last `window` ones (window > 0).  sink_logits: NULL, or float32 [Hq], one more logit per query head that has no value
- * (natural-log units).  A sequence of length 0 yields zeros.  Sums, softmax statistics and accumulators are binary32.  The
- * weights that meet the codes have 22 bits for float32 outputs, 12 for bf16 ones; for these a logit may be off by 2^-8 (some 2^-11 as
- * measured) of what one step of a key's code moves it by in the query's largest channel.
+ * (natural-log units).  A sequence of length 0 yields zeros.  Sums, softmax statistics and accumulators are binary32.  Two things
+ * are shorter.  A weight times its token's scale is rounded to 22 bits for float32 outputs and 11 for bf16 ones, or to 2^-34 of the
+ * largest weight times the largest scale of the sequence where that is coarser; and for bf16 outputs a logit may be off by 2^-8 (some
+ * 2^-11 as measured) of what one step of a key's code moves it by in the query's largest channel.  A query's coordinates are taken
+ * exactly down to 2^-27 of the largest one among the heads of its KV head, and to 2^-35 of it below.
  *   q    bf16 [batch][Hq][d], 16-byte aligned
  *   out  [batch][Hq][d], float32 if out_is_fp32 (8-byte aligned) else bf16 (4-byte aligned)
  *   workspace  novakv_int4_workspace_bytes(ctx, batch) bytes, 256-byte aligned; contents are scratch, which calls that may overlap

@@ -10,8 +10,8 @@
 //    (tcgen05 wants its operands as 16-bit tiles in shared memory: the unpacked codes would have to be written there first,
 //    four times the bytes of the cache).  A code c is the binary16 subnormal c 2^-24, which the tensor core multiplies exactly:
 //    one AND of a word gives two operands, no conversion.  Codes in bits 4..7 are 16 c; what they meet carries a 1/16.
-//  * Exactness: q is a bfloat16 number, exact in binary16 after a power of two; accumulators, softmax statistics and the zeros'
-//    share are binary32.  What the weights are rounded to goes by the output's type (FINE below).
+//  * Exactness: q is a bfloat16 number, exact in binary16 after a power of two (but for what is 2^-27 of the KV head's largest);
+//    accumulators, softmax statistics and the zeros' share are binary32.  What the weights are rounded to goes by the output's type (FINE below).
 //  * Streaming: the walk over (sequence, KV head, unit of 32 tokens at d = 128, 64 at d = 64) is cut evenly among the CTAs (one
 //    per SM) and again among their 16 warps; each warp copies its units' keys and values (a bulk copy each) into a ring of its
 //    own, a unit ahead of the one it works on, and no warp waits for another before the end.  (A page, 64 tokens, is 4.6 KB of a
@@ -36,7 +36,9 @@ constexpr int SLOTS = 2;                     // ring of a warp, in units (keys a
 // tokens (d = 128, 8 KV heads): 57.4 us at 0, 52.4 at 1, 50.8 at 2, 49.6 at 3, 50.1 at 5; 8 x 16384 tokens 36.5 to 37 throughout.
 constexpr int PAIR_COST = 3;
 constexpr int HEADROOM = 4;                  // a new maximum is set this many bits high: the next records need no rescaling
-constexpr float W_ONE = 32768.f;             // the weight 1 in binary16: what underflows is 2^-39 of the largest
+// The weight 1 at the largest scale so far, in binary16, once that scale is a quarter to a half of its power of two: what lies below
+// 2^-34 of the largest weight (HEADROOM below 1) times that scale is cut off.
+constexpr float W_ONE = 32768.f;
 
 template <int D, int HG>
 struct Plan {
@@ -416,7 +418,8 @@ novakv_int4_decode_kernel(const DecodeArgs a) {
             if (!(mx < CUDART_INF_F)) mx = 0.f;                   // (a head with an infinity does not decide for the others)
 #pragma unroll
             for (int s = 4; s < 32; s <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
-            // 2^e brings the heads' largest coordinate just below 2^15 (what is 2^-31 of it or less loses bits)
+            // 2^e brings the heads' largest coordinate just below 2^15: their eight bits fit down to 2^-31 of it, 2^-27
+            // where a sixteenth of them is taken
             const int e = min(15 - ((int)(__float_as_uint(mx) >> 23) - 126), 120);
             const float f = __uint_as_float((uint32_t)(e + 127) << 23), odd = FINE ? f : f * 0.0625f;
             float sum[G];

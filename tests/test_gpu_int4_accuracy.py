@@ -71,3 +71,23 @@ def test_float32_outputs(contexts, shape, n, ctas, std):
     o32, _ = A.attention(q[0], k, v, shape[2] ** -0.5, torch.float32, sink=sink)
     error, bound = A.rms(out[0].double() - o), A.float32_bound(o, o32, p, v)
     assert error <= bound, (error, bound, A.rms(o))
+
+
+@pytest.mark.parametrize("std", [3.0, 10.0, 30.0])
+@pytest.mark.parametrize("n", [40, 777, 32768])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_bf16_outputs(contexts, shape, n, std):
+    """Logits that matter one by one.  Each is a sum of d products that are cut off at 2^-15 of a step of the key's code in the query's
+    largest channel, 136 times with either sign: sqrt(136) 2^-15 in the mean at most, 2^-11 here, times half a group's range."""
+    ctx = contexts(shape)
+    cache, k, v, g = filled(ctx, n, 82)
+    q = (std * torch.randn((1, shape[0], shape[2]), generator=g, device="cuda")).to(torch.bfloat16)
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    cache.decode(q, out=out)
+    scale = shape[2] ** -0.5
+    o, p = A.attention(q[0], k, v, scale)
+    half = lambda x: (lambda y: (y.amax(-1) - y.amin(-1)) / 2)(x.double().unflatten(-1, (-1, 64)))  # noqa: E731
+    logit = 2.0 ** -11 * scale * q.abs().max().item() * (half(k) / 7.5).max().item()
+    moved = logit * torch.einsum("hgn,nhc->hgc", p ** 2, half(v) ** 2).mean().sqrt().item()
+    error, bound = A.rms(out[0].double() - o), (A.bf16_bound(o, p, v) ** 2 + moved ** 2) ** 0.5
+    assert error <= bound, (error, bound, A.rms(o))

@@ -24,3 +24,29 @@ def test_queries_of_any_exponent(contexts, shape, exponent, dtype):  # noqa: F81
     bound = A.float32_bound(o, o32, p, v) if dtype == torch.float32 else A.bf16_bound(o, p, v)
     error = A.rms(out[0].double() - o)
     assert error <= bound, (error, bound, A.rms(o))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("small", [0, 1])
+@pytest.mark.parametrize("shape", [(32, 8, 128), (16, 16, 128)])
+def test_groups_of_channels_of_two_sizes(contexts, shape, small, dtype):  # noqa: F811
+    """Values of 64 channels 2^10 times as large as those of the other 64: each group is as exact as if it were alone."""
+    from paper_2608_04074_b200.runtime import Int4Cache
+    ctx, n = contexts(shape), 3000
+    g = torch.Generator(device="cuda").manual_seed(96)
+    k, v = (torch.randn((n, shape[1], 128), generator=g, device="cuda") for _ in range(2))
+    v[..., 64 * small:64 * small + 64] *= 2.0 ** -10
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    cache = Int4Cache(ctx, 1, n)
+    cache.append(None, k.to(torch.bfloat16), v.to(torch.bfloat16), torch.zeros_like(pos), pos)
+    k, v = cache.gather(torch.zeros_like(pos), pos, torch.float32)
+    q = torch.randn((1, shape[0], 128), generator=g, device="cuda").to(torch.bfloat16)
+    out = torch.empty(q.shape, dtype=dtype, device="cuda")
+    cache.decode(q, out=out)
+    o, p = A.attention(q[0], k, v, 128 ** -0.5)
+    o32, _ = A.attention(q[0], k, v, 128 ** -0.5, torch.float32)
+    for c in (slice(0, 64), slice(64, 128)):
+        part = (o[:, c], o32[:, c], p, v[..., c]) if dtype == torch.float32 else (o[:, c], p, v[..., c])
+        bound = (A.float32_bound if dtype == torch.float32 else A.bf16_bound)(*part)
+        error = A.rms(out[0, :, c].double() - o[:, c])
+        assert error <= bound, (c, error, bound, A.rms(o[:, c]))
