@@ -50,3 +50,38 @@ def test_groups_of_channels_of_two_sizes(contexts, shape, small, dtype):  # noqa
         bound = (A.float32_bound if dtype == torch.float32 else A.bf16_bound)(*part)
         error = A.rms(out[0, :, c].double() - o[:, c])
         assert error <= bound, (c, error, bound, A.rms(o[:, c]))
+
+
+def test_scales_are_products_not_quotients(contexts):  # noqa: F811
+    """Keys of groups whose range times the binary32 number next to 1/15 and whose range divided by 15 round to different scales:
+    the cache holds the product."""
+    import numpy as np
+
+    import cache_reference as R
+    from paper_2608_04074_b200 import cache_format
+    from paper_2608_04074_b200.binding import QKTransform
+    ctx, gen = contexts((4, 1, 64)), np.random.default_rng(97)
+    w = R.to_bf16(1 + 0.3 * gen.normal(size=64))
+    rows = []
+    for _ in range(40):
+        k = R.to_bf16(gen.normal(size=(50000, 1, 64)))
+        x = R.transform(k, np.zeros(len(k)), weight=w)[0].astype(np.float32)
+        span = x.max(-1) - R.to_bf16(x.min(-1))
+        apart = R.to_bf16(span * (np.float32(1) / np.float32(15))) != R.to_bf16(span / np.float32(15))
+        rows.append(k[apart[:, 0]])
+        if sum(map(len, rows)) >= 3:
+            break
+    k = np.concatenate(rows)
+    n = len(k)
+    assert 3 <= n <= 64
+    x = R.transform(k, np.zeros(n), weight=w)[0].astype(np.float32)
+    codes, scale, zero = R.quantise(x)
+    dev = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    pools = [torch.zeros((1, ctx.novakv_int4_page_bytes()), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    kd = dev(k).to(torch.bfloat16)
+    ctx.novakv_int4_append(QKTransform(k_weight=dev(w).to(torch.bfloat16)), kd, kd, dev(np.zeros(n, np.int32)), dev(np.arange(n, dtype=np.int32)), *pools,
+                           dev(np.zeros((1, 1), np.int32)), torch.zeros(1, dtype=torch.int32, device="cuda"))
+    c, s, z = cache_format.int4_read_tokens(pools[0].cpu().numpy(), np.zeros(1, np.int32), 1, 64, 0, n)
+    assert np.array_equal(s, scale) and np.array_equal(z, zero) and np.array_equal(c, codes)
+    span = x.max(-1) - zero[..., 0]
+    assert np.array_equal(s[..., 0], R.to_bf16(span * (np.float32(1) / np.float32(15)))) and (s[..., 0] != R.to_bf16(span / np.float32(15))).all()
