@@ -249,7 +249,8 @@ class BandedCache:
 
 
 class _RowCache:
-    """Page table, lengths and pools of a cache whose append takes the projection's rows (keys through a ``QKTransform``)."""
+    """Page table, lengths and pools of a cache whose append takes the projection's rows (keys through a ``QKTransform``).  A token
+    behind its sequence's capacity is skipped, with a status bit."""
 
     def __init__(self, ctx: Context, batch: int, capacity_tokens, seed: int = 0):
         self.ctx, self.batch = ctx, batch
@@ -257,7 +258,8 @@ class _RowCache:
         cap = np.maximum(np.broadcast_to(np.asarray(capacity_tokens, np.int32), (batch,)), 1)
         table, n_pages = synth.shuffled_page_table(seed, cap, cache_format.PAGE_TOKENS)
         self.n_pages, self.page_table_host = int(n_pages), table
-        self.page_table = torch.from_numpy(np.where(table < 0, 0, table).astype(np.int32)).to(self.device)
+        # (-1 behind a sequence's pages: an append beyond its capacity is skipped and reported)
+        self.page_table = torch.from_numpy(table).to(self.device)
         self.seq_lens = torch.zeros(batch, dtype=torch.int32, device=self.device)
 
     def _q_out(self, q, q_out):
