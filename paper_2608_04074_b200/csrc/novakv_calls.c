@@ -7,6 +7,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <dlfcn.h>
+#include <limits.h>
 #include <stdint.h>
 
 #include "novakv.h"
@@ -351,7 +352,7 @@ static PyObject* operator_call(PyObject* self, PyObject* const* args, size_t nar
     }
     const long long n = first[0], table_rows = first[1], pool_pages = first[2];
     if (op == INT4_DECODE && n != table_rows) { refuse(op, operators[op].table, "has to have one row for each query"); return NULL; }
-    if (n > 0x7fffffff || pool_pages > 0x7fffffff) { refuse(op, 0, "is too large"); return NULL; }
+    if (n > INT_MAX || pool_pages > INT_MAX) { refuse(op, 0, "is too large"); return NULL; }
     long long a[MAX_ARGS];
     float f = 0.f;
     const param* p = operators[op].p;
@@ -378,9 +379,14 @@ static PyObject* operator_call(PyObject* self, PyObject* const* args, size_t nar
                 a[i] = n > 1 ? z[arg].stride[0] : e->hq * e->d;        /* (of a single row any stride is one) */
                 break;
             case 'N': a[i] = n; break;
-            case '0': a[i] = z[arg].size[0]; break;
-            case '1': a[i] = z[arg].size[1]; break;
-            case 'I': if (as_int(x, 0, &a[i])) return NULL; break;
+            case '0': case '1':                            /* (what the C call takes as an int) */
+                a[i] = z[arg].size[p[i].kind - '0'];
+                if (a[i] > INT_MAX) { refuse(op, arg, "is too large"); return NULL; }
+                break;
+            case 'I':
+                if (as_int(x, 0, &a[i])) return NULL;
+                if (a[i] > INT_MAX || a[i] < INT_MIN) { refuse(op, arg, "is out of range"); return NULL; }
+                break;
             case 'F': f = (float)PyFloat_AsDouble(x); break;
             case 'T': a[i] = is_dtype(x, float32, float32); break;
             case 'B': { PyObject* b = PyObject_GetAttr(x, s_nbytes); if (!b) return NULL; a[i] = PyLong_AsLongLong(b); Py_DECREF(b); break; }
