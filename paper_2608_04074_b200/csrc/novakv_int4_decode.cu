@@ -19,9 +19,10 @@
 //  * Join: what a warp has of a (sequence, KV head) pair that it does not hold whole goes to shared memory; the CTA joins these
 //    pieces, and a second kernel joins the at most two per CTA that reach over its ends.
 //
-// B200, bf16 output, 6.56 TB/s of measured copy bandwidth: 64 x 16384 tokens (32 / 8 heads, d = 128) 193 us, 96 % of it; 8 x 16384 37 us,
-// 63 %, of which launches, the look-up of the first units and the join are 8; 16 x 65536 (64 / 8 heads, d = 64) 115 us, 80 %, and more where
-// it runs for seconds and the board's power limit takes the clock down: what is left is instructions.
+// B200, bf16 output, 6.56 TB/s of measured copy bandwidth: 64 x 16384 tokens (32 / 8 heads, d = 128) 193 to 197 us, 94 to 96 % of it; 8 x 16384
+// 37 us, 62 %, of which launches, the look-up of the first units and the join are 8; 16 x 65536 (64 / 8 heads, d = 64) 115 us, 80 %, and
+// 134 where it runs for seconds and the board's power limit takes the clock from 1.96 to 1.67 GHz: what is left is instructions (680 a unit,
+// set-up and join included; 580 at d = 128).
 #include <math_constants.h>
 
 #include "novakv_int4.cuh"
@@ -33,7 +34,7 @@ namespace {
 constexpr int WARPS = 16, THREADS = WARPS * 32;
 constexpr int SLOTS = 2;                     // ring of a warp, in units (keys and values)
 // What setting up and writing out a (sequence, KV head) pair weighs in units, when the walk is cut.  32 sequences of 163 to 32768
-// tokens (d = 128, 8 KV heads): 57.4 us at 0, 52.4 at 1, 50.8 at 2, 49.6 at 3, 50.1 at 5; 8 x 16384 tokens 36.5 to 37 throughout.
+// tokens (d = 128, 8 KV heads): 60.3 us at 0, 55.3 at 1, 51.6 at 2, 50.6 at 3, 50.9 at 5; 8 x 16384 tokens 37.4, 36.6, 36.3, 36.2, 36.2.
 constexpr int PAIR_COST = 3;
 constexpr int HEADROOM = 4;                  // a new maximum is set this many bits high: the next records need no rescaling
 // The weight 1 at the largest scale so far, in binary16, once that scale is a quarter to a half of its power of two: what lies below
@@ -893,8 +894,9 @@ novakv_int4_merge_kernel(const DecodeArgs a) {
 }
 
 // Units of a warp up to which a CTA keeps a pair to itself.  One sequence, 8 pairs, one CTA each / split over all and joined:
-// d = 128, 777 tokens (2 units a warp) 8.6 / 11.7 us, 1500 (3) 10.7 / 11.9, 2048 (4) 12.4 / 12.8, 4096 (8) 18.6 / 12.4;
-// d = 64, 700 tokens (1) 6.0 / 9.6, 2000 (2) 8.8 / 10.7, 4000 (4) 12.3 / 11.6.
+// d = 128, 777 tokens (2 units a warp) 9.0 / 10.9 us, 1500 (3) 11.2 / 11.0, 2048 (4) 12.9 / 11.7, 4096 (8) 19.4 / 11.2;
+// d = 64, 700 tokens (1) 6.0 / 9.4, 2000 (2) 8.7 / 10.0, 4000 (4) 12.5 / 10.8.  (The host goes by what a sequence can have: the table's width
+// and the window.  A short sequence behind a wide table takes the second form.)
 constexpr int ONE_UNITS = 3;
 int scan_ctas(const novakv_ctx* ctx) { return ctx->scan_ctas > 0 && ctx->scan_ctas < ctx->n_sm ? ctx->scan_ctas : ctx->n_sm; }
 size_t info_bytes(const novakv_ctx* ctx) { return ((size_t)ctx->n_sm * 2 * sizeof(int) + 255) & ~(size_t)255; }
