@@ -85,3 +85,34 @@ def test_scales_are_products_not_quotients(contexts):  # noqa: F811
     assert np.array_equal(s, scale) and np.array_equal(z, zero) and np.array_equal(c, codes)
     span = x.max(-1) - zero[..., 0]
     assert np.array_equal(s[..., 0], R.to_bf16(span * (np.float32(1) / np.float32(15)))) and (s[..., 0] != R.to_bf16(span / np.float32(15))).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("ctas", [0, 1])
+@pytest.mark.parametrize("run", ["rising", "falling", "mixed"])
+@pytest.mark.parametrize("shape", [(32, 8, 128), (64, 8, 64), (4, 2, 64)])
+def test_scales_over_a_sequence(contexts, shape, run, ctas, dtype):  # noqa: F811
+    """Values that grow or shrink by 2^16 over a sequence, or differ by as much from token to token: sums are brought along."""
+    from paper_2608_04074_b200.runtime import Int4Cache
+    ctx, n = contexts(shape), 3000
+    g = torch.Generator(device="cuda").manual_seed(98)
+    k, v = (torch.randn((n, shape[1], shape[2]), generator=g, device="cuda") for _ in range(2))
+    exponent = {"rising": torch.linspace(-8, 8, n, device="cuda"), "falling": torch.linspace(8, -8, n, device="cuda"),
+                "mixed": torch.randint(-8, 9, (n,), generator=g, device="cuda").float()}[run]
+    v = v * torch.exp2(exponent)[:, None, None]
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    cache = Int4Cache(ctx, 1, n)
+    cache.append(None, k.to(torch.bfloat16), v.to(torch.bfloat16), torch.zeros_like(pos), pos)
+    k, v = cache.gather(torch.zeros_like(pos), pos, torch.float32)
+    q = torch.randn((1, shape[0], shape[2]), generator=g, device="cuda").to(torch.bfloat16)
+    out = torch.empty(q.shape, dtype=dtype, device="cuda")
+    try:
+        ctx.novakv_debug_set_scan_ctas(ctas)
+        cache.decode(q, out=out)
+    finally:
+        ctx.novakv_debug_set_scan_ctas(0)
+    o, p = A.attention(q[0], k, v, shape[2] ** -0.5)
+    o32, _ = A.attention(q[0], k, v, shape[2] ** -0.5, torch.float32)
+    bound = A.float32_bound(o, o32, p, v) if dtype == torch.float32 else A.bf16_bound(o, p, v)
+    error = A.rms(out[0].double() - o)
+    assert error <= bound, (error, bound, A.rms(o))
